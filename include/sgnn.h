@@ -53,6 +53,15 @@ enum {
                             the sparse product at width d_out; worth it when d_out < d_in           */
 };
 
+/* activations of the feed-forward operators (sgnn_linear_fwd, sgnn_glu_fwd) */
+enum {
+    SGNN_ACT_NONE = 0,
+    SGNN_ACT_RELU = 1,
+    SGNN_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution function (by the error function)          */
+    SGNN_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2                                */
+    SGNN_ACT_SILU = 4       /* z / (1 + exp(-z))                                                              */
+};
+
 typedef struct sgnn_ctx sgnn_ctx;
 typedef void *sgnn_stream; /* hipStream_t */
 
@@ -407,6 +416,90 @@ int sgnn_sgd_step(sgnn_ctx *ctx, float *w, const float *g, int64_t n, double lr,
                   sgnn_stream stream);
 int sgnn_adam_step(sgnn_ctx *ctx, float *w, const float *g, float *m, float *v, int64_t n, double lr,
                    double beta1, double beta2, double eps, int64_t t, sgnn_stream stream);
+
+/*
+ * Feed-forward block of a layer: products with activation and residual, a gated projection, and the norms around a block.
+ *
+ * Matrices are SGNN_F32, with products in fp32 precision, or with SGNN_BF16_MFMA (the only flag) each SGNN_F32 or SGNN_BF16 as the caller
+ * likes: product operands are rounded to bfloat16 (nearest even), sums, activations and statistics are fp32, a result is rounded once as it is
+ * stored.  SGNN_BF16 anywhere without the flag is SGNN_ERR_UNSUPPORTED.  Vectors (biases, scales, their gradients) are fp32.  Any width from
+ * 1 to 2^24, any leading dimension and alignment; bfloat16 operands whose columns and leading dimension are multiples of 8 and that start on 16
+ * bytes are read as they lie, others through a copy in the context scratch.  No row_index.  A batch of 0 rows is valid: its matrices may have
+ * null pointers, forward calls do nothing, backward calls write zero gradients for weights and vectors.  Outputs must not
+ * overlap other arguments except where said; gradients are overwritten, not added to, and every call is bit-reproducible.
+ */
+
+/*
+ * Scratch for the calls below on up to `rows` rows, weights of up to d_in x d_out (both projections of sgnn_glu_*) and norms of rows of up to
+ * max(d_in, d_out) values.  Like sgnn_ctx_reserve it allocates, synchronises the device when it has to grow, and never shrinks: the larger of the two
+ * reservations holds.  Growing frees the old scratch: do it before capturing calls of this context into a HIP graph.
+ */
+int sgnn_ctx_reserve_ffn(sgnn_ctx *ctx, uint64_t rows, uint32_t d_in, uint32_t d_out);
+
+/*
+ * Y = act(Z) + R,  Z = X W + bias.
+ *   X  M x K;  W  K x N;  bias fp32[N] or NULL;  act SGNN_ACT_*;  R  M x N or NULL, may be Y itself (same storage and leading dimension)
+ *   Y  out M x N;  Z  out M x N or NULL: the pre-activation, kept by the caller for sgnn_linear_bwd
+ */
+int sgnn_linear_fwd(sgnn_ctx *ctx, const sgnn_mat *X, const sgnn_mat *W, const float *bias, int act, int flags,
+                    const sgnn_mat *R, sgnn_mat *Y, sgnn_mat *Z, sgnn_stream stream);
+
+/*
+ * Its backward pass: dZ = dY * act'(Z);  dX = dZ W^T;  dW = X^T dZ;  dbias = column sums of dZ.  The gradient of R is dY itself.
+ *   Z  as kept (NULL allowed for SGNN_ACT_NONE);  dX M x K, dW K x N, dbias fp32[N]: out, or NULL where not wanted
+ * ReLU's derivative at 0 is 0.  With SGNN_BF16_MFMA dZ is rounded to bfloat16 for the products, dbias is summed before that.
+ */
+int sgnn_linear_bwd(sgnn_ctx *ctx, const sgnn_mat *X, const sgnn_mat *W, const sgnn_mat *Z, int act, int flags,
+                    const sgnn_mat *dY, sgnn_mat *dX, sgnn_mat *dW, float *dbias, sgnn_stream stream);
+
+/*
+ * Gated projection: H = act(G) * U,  G = X Wg + bg,  U = X Wu + bu, both products in one kernel.
+ *   X  M x K;  Wg, Wu  K x N;  bg, bu fp32[N] or NULL;  H  out M x N;  G, U  out M x N or NULL: kept for sgnn_glu_bwd
+ */
+int sgnn_glu_fwd(sgnn_ctx *ctx, const sgnn_mat *X, const sgnn_mat *Wg, const sgnn_mat *Wu, const float *bg, const float *bu,
+                 int act, int flags, sgnn_mat *H, sgnn_mat *G, sgnn_mat *U, sgnn_stream stream);
+
+/*
+ * Its backward pass: dG = dH * U * act'(G), dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG, dWu = X^T dU;
+ * dbg, dbu their column sums.  Outputs may be NULL where not wanted; rounding as in sgnn_linear_bwd.
+ */
+int sgnn_glu_bwd(sgnn_ctx *ctx, const sgnn_mat *X, const sgnn_mat *Wg, const sgnn_mat *Wu, const sgnn_mat *G, const sgnn_mat *U,
+                 int act, int flags, const sgnn_mat *dH, sgnn_mat *dX, sgnn_mat *dWg, sgnn_mat *dWu, float *dbg, float *dbu,
+                 sgnn_stream stream);
+
+/*
+ * The norm behind a block, the block's way into the residual stream, and the norm in front of the next block, one kernel:
+ *   b = gamma_post n(Z) (post) or Z;   Y = res_scale X + col_scale sigmoid(gate) b;   N = gamma_pre n(Y)
+ *   n(v)_j = v_j / sqrt(mean_j v_j^2 + eps), of Y before it is rounded for storage
+ * Rows of up to 16384 values (wider ones are SGNN_ERR_UNSUPPORTED).  Storage of every matrix as it likes, without a flag.
+ */
+typedef struct {
+    const sgnn_mat *gate;     /* M x d, or M x 1: one for the row; gate logits, NULL: no gate                    */
+    const float *gamma_post;  /* fp32[d] or NULL (ones); only with post                                         */
+    const float *col_scale;   /* fp32[d] or NULL (ones): residual scale of each column                          */
+    const float *gamma_pre;   /* fp32[d] or NULL (ones)                                                         */
+    float res_scale;          /* factor of X                                                                    */
+    float eps;                /* >= 0, of both norms                                                            */
+    int post;                 /* 1: Z goes through the norm                                                     */
+} sgnn_block_norm;
+
+/*
+ *   X  M x d, the residual stream;  Z  M x d, the block's output, or NULL: no block yet (Y = res_scale X, N its norm)
+ *   Y  out M x d or NULL, may be X itself (same storage and leading dimension);  N  out M x d or NULL: without it the second norm is not taken
+ *   inv_rms_post, inv_rms_pre  out fp32[M] or NULL: 1 / sqrt(mean + eps) of the norms that are taken, kept for the backward pass
+ */
+int sgnn_block_norm_fwd(sgnn_ctx *ctx, const sgnn_mat *X, const sgnn_mat *Z, const sgnn_block_norm *p, sgnn_mat *Y, sgnn_mat *N,
+                        float *inv_rms_post, float *inv_rms_pre, sgnn_stream stream);
+
+/*
+ * Its backward pass from the kept Z, Y (needed with dN) and inverse roots:
+ *   dY  M x d: the gradient that reaches Y from elsewhere, or NULL (zero);  dN  M x d or NULL: no second norm;  one of them is needed
+ *   dX, dZ  out M x d, dgate  out, shaped like the gate, dgamma_post, dscale, dgamma_pre  out fp32[d]; each may be NULL
+ * dX may be dY itself, dZ may be dN itself (same storage and leading dimension).
+ */
+int sgnn_block_norm_bwd(sgnn_ctx *ctx, const sgnn_mat *Z, const sgnn_mat *Y, const sgnn_block_norm *p, const float *inv_rms_post,
+                        const float *inv_rms_pre, const sgnn_mat *dY, const sgnn_mat *dN, sgnn_mat *dX, sgnn_mat *dZ,
+                        sgnn_mat *dgate, float *dgamma_post, float *dscale, float *dgamma_pre, sgnn_stream stream);
 
 /* Plain operators, exported for tests and for callers that build their own layer. */
 

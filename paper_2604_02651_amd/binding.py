@@ -22,6 +22,11 @@ SGNN_DY_MASKED = 8
 SGNN_FUSE_TAIL = 16
 SGNN_F32 = 0
 SGNN_BF16 = 1
+SGNN_ACT_NONE = 0
+SGNN_ACT_RELU = 1
+SGNN_ACT_GELU = 2
+SGNN_ACT_GELU_TANH = 3
+SGNN_ACT_SILU = 4
 
 _ERR_NAMES = {-1: "SGNN_ERR_INVALID_ARG", -2: "SGNN_ERR_CAPACITY", -3: "SGNN_ERR_UNSUPPORTED", -4: "SGNN_ERR_HIP",
               -5: "SGNN_ERR_INTERNAL"}
@@ -47,6 +52,11 @@ class _Csr(C.Structure):
 class _Mat(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64),
                 ("row_index", C.c_void_p)]
+
+
+class _BlockNorm(C.Structure):
+    _fields_ = [("gate", C.POINTER(_Mat)), ("gamma_post", C.c_void_p), ("col_scale", C.c_void_p), ("gamma_pre", C.c_void_p),
+                ("res_scale", C.c_float), ("eps", C.c_float), ("post", C.c_int)]
 
 
 _lib = None
@@ -104,7 +114,16 @@ def lib():
         L.sgnn_spmm.argtypes = [vp, C.POINTER(_Csr), C.POINTER(_Mat), C.POINTER(_Mat), C.POINTER(_Mat), vp]
         L.sgnn_copy_f32.argtypes = [vp, vp, vp, i64, vp]
         L.sgnn_gemm.argtypes = [vp, ci, ci, i64, i64, i64, vp, ci, i64, vp, ci, i64, vp, ci, vp, ci, i64, vp, ci, i64, vp, vp]
-        for name in ("sgnn_ctx_create", "sgnn_ctx_destroy", "sgnn_ctx_reserve", "sgnn_ctx_status",
+        pm = C.POINTER(_Mat)
+        L.sgnn_ctx_reserve_ffn.argtypes = [vp, u64, u32, u32]
+        L.sgnn_linear_fwd.argtypes = [vp, pm, pm, vp, ci, ci, pm, pm, pm, vp]
+        L.sgnn_linear_bwd.argtypes = [vp, pm, pm, pm, ci, ci, pm, pm, pm, vp, vp]
+        L.sgnn_glu_fwd.argtypes = [vp, pm, pm, pm, vp, vp, ci, ci, pm, pm, pm, vp]
+        L.sgnn_glu_bwd.argtypes = [vp, pm, pm, pm, pm, pm, ci, ci, pm, pm, pm, pm, vp, vp, vp]
+        L.sgnn_block_norm_fwd.argtypes = [vp, pm, pm, C.POINTER(_BlockNorm), pm, pm, vp, vp, vp]
+        L.sgnn_block_norm_bwd.argtypes = [vp, pm, pm, C.POINTER(_BlockNorm), vp, vp, pm, pm, pm, pm, pm, vp, vp, vp, vp]
+        for name in ("sgnn_ctx_reserve_ffn", "sgnn_linear_fwd", "sgnn_linear_bwd", "sgnn_glu_fwd", "sgnn_glu_bwd", "sgnn_block_norm_fwd", "sgnn_block_norm_bwd",
+                     "sgnn_ctx_create", "sgnn_ctx_destroy", "sgnn_ctx_reserve", "sgnn_ctx_status",
                      "sgnn_ctx_profile", "sgnn_ctx_profile_read",
                      "sgnn_sample_uniform", "sgnn_induced_csr", "sgnn_csr_plan", "sgnn_gather_rows", "sgnn_gcn_fwd", "sgnn_gcn_bwd", "sgnn_tail_fwd", "sgnn_tail_bwd", "sgnn_gemm_tail_fwd", "sgnn_sgd_step", "sgnn_adam_step", "sgnn_graph_normalized_csr", "sgnn_induced_csr_range", "sgnn_csr_transpose", "sgnn_sigmoid_bce", "sgnn_colsum",
                      "sgnn_softmax_xent", "sgnn_spmm_xent", "sgnn_spmm", "sgnn_gemm", "sgnn_copy_f32"):
@@ -160,6 +179,10 @@ class Context:
 
     def reserve(self, N: int, E: int, B: int, d_max: int, max_entries: int = 0):
         self.check(lib().sgnn_ctx_reserve(self._h, N, E, B, d_max, max_entries))
+
+    def reserve_ffn(self, rows: int, d_in: int, d_out: int):
+        """Scratch for the feed-forward operators: up to `rows` rows, weights of up to d_in x d_out."""
+        self.check(lib().sgnn_ctx_reserve_ffn(self._h, rows, d_in, d_out))
 
     def status(self, stream=None):
         self.check(lib().sgnn_ctx_status(self._h, _stream(stream)))
@@ -509,6 +532,88 @@ def sgnn_gemm(ctx: Context, trans_a: bool, trans_b: bool, A: torch.Tensor, B: to
                               _ptr(Cm, None, "C"), _dt(Cm, "C"), Cm.stride(0), _ptr(mask, None, "mask"), _dt(mask, "mask"),
                               mask.stride(0) if mask is not None else 0, _ptr(b_colsum, torch.float32, "b_colsum"),
                               _stream(stream)))
+
+
+# ---- feed-forward operators ----------------------------------------------------------------------
+
+def _m(t: Optional[torch.Tensor], name: str):
+    """A matrix of either storage type, or None."""
+    return None if t is None else C.byref(_mat(t, None, name, allow_bf16=True))
+
+
+def _vec(t: Optional[torch.Tensor], n: int, name: str):
+    if t is None:
+        return None
+    if t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % name)
+    return _ptr(t, torch.float32, name)
+
+
+def sgnn_linear_fwd(ctx: Context, X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], act: int, flags: int, Y: torch.Tensor,
+                    R: Optional[torch.Tensor] = None, Z: Optional[torch.Tensor] = None, stream=None):
+    """Y = act(X W + bias) + R; Z, if given, receives X W + bias for sgnn_linear_bwd.  R may be Y."""
+    ctx.check(lib().sgnn_linear_fwd(ctx._h, _m(X, "X"), _m(W, "W"), _vec(bias, W.shape[1], "bias"), act, flags, _m(R, "R"), _m(Y, "Y"), _m(Z, "Z"),
+                                    _stream(stream)))
+
+
+def sgnn_linear_bwd(ctx: Context, X: torch.Tensor, W: torch.Tensor, Z: Optional[torch.Tensor], act: int, flags: int, dY: torch.Tensor,
+                    dX: Optional[torch.Tensor], dW: Optional[torch.Tensor], dbias: Optional[torch.Tensor], stream=None):
+    """dZ = dY act'(Z); dX = dZ W^T, dW = X^T dZ, dbias = column sums of dZ; None where not wanted."""
+    ctx.check(lib().sgnn_linear_bwd(ctx._h, _m(X, "X"), _m(W, "W"), _m(Z, "Z"), act, flags, _m(dY, "dY"), _m(dX, "dX"), _m(dW, "dW"),
+                                    _vec(dbias, W.shape[1], "dbias"), _stream(stream)))
+
+
+def sgnn_glu_fwd(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor], bu: Optional[torch.Tensor], act: int,
+                 flags: int, H: torch.Tensor, G: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None, stream=None):
+    """H = act(X Wg + bg) * (X Wu + bu); G, U, if given, receive the two projections for sgnn_glu_bwd."""
+    n = Wg.shape[1]
+    ctx.check(lib().sgnn_glu_fwd(ctx._h, _m(X, "X"), _m(Wg, "Wg"), _m(Wu, "Wu"), _vec(bg, n, "bg"), _vec(bu, n, "bu"), act, flags, _m(H, "H"), _m(G, "G"),
+                                 _m(U, "U"), _stream(stream)))
+
+
+def sgnn_glu_bwd(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: torch.Tensor, U: torch.Tensor, act: int, flags: int,
+                 dH: torch.Tensor, dX: Optional[torch.Tensor], dWg: Optional[torch.Tensor], dWu: Optional[torch.Tensor],
+                 dbg: Optional[torch.Tensor] = None, dbu: Optional[torch.Tensor] = None, stream=None):
+    """dG = dH U act'(G), dU = dH act(G); dX = dG Wg^T + dU Wu^T, dWg = X^T dG, dWu = X^T dU and the column sums of dG, dU; None where
+    not wanted."""
+    n = Wg.shape[1]
+    ctx.check(lib().sgnn_glu_bwd(ctx._h, _m(X, "X"), _m(Wg, "Wg"), _m(Wu, "Wu"), _m(G, "G"), _m(U, "U"), act, flags, _m(dH, "dH"), _m(dX, "dX"),
+                                 _m(dWg, "dWg"), _m(dWu, "dWu"), _vec(dbg, n, "dbg"), _vec(dbu, n, "dbu"), _stream(stream)))
+
+
+def _block_norm(d: int, gate, gamma_post, col_scale, gamma_pre, res_scale: float, eps: float, post: bool) -> _BlockNorm:
+    g = C.pointer(_mat(gate, None, "gate", allow_bf16=True)) if gate is not None else None
+    return _BlockNorm(g, _vec(gamma_post, d, "gamma_post"), _vec(col_scale, d, "col_scale"), _vec(gamma_pre, d, "gamma_pre"), res_scale, eps, int(post))
+
+
+def sgnn_block_norm_fwd(ctx: Context, X: torch.Tensor, Z: Optional[torch.Tensor], gate: Optional[torch.Tensor], gamma_post: Optional[torch.Tensor],
+                        col_scale: Optional[torch.Tensor], gamma_pre: Optional[torch.Tensor], res_scale: float, post: bool, eps: float,
+                        Y: Optional[torch.Tensor], N: Optional[torch.Tensor], inv_rms_post: Optional[torch.Tensor] = None,
+                        inv_rms_pre: Optional[torch.Tensor] = None, stream=None):
+    """Y = res_scale X + col_scale sigmoid(gate) b, b = gamma_post rmsnorm(Z) (post) or Z; N = gamma_pre rmsnorm(Y).  gate: a matrix like Z or one
+    column.  inv_rms_*: kept for sgnn_block_norm_bwd.  Y may be X."""
+    p = _block_norm(X.shape[1], gate, gamma_post, col_scale, gamma_pre, res_scale, eps, post)
+    ctx.check(lib().sgnn_block_norm_fwd(ctx._h, _m(X, "X"), _m(Z, "Z"), C.byref(p), _m(Y, "Y"), _m(N, "N"), _vec(inv_rms_post, X.shape[0], "inv_rms_post"),
+                                        _vec(inv_rms_pre, X.shape[0], "inv_rms_pre"), _stream(stream)))
+
+
+def sgnn_block_norm_bwd(ctx: Context, Z: Optional[torch.Tensor], Y: Optional[torch.Tensor], gate: Optional[torch.Tensor],
+                        gamma_post: Optional[torch.Tensor], col_scale: Optional[torch.Tensor], gamma_pre: Optional[torch.Tensor], res_scale: float,
+                        post: bool, inv_rms_post: Optional[torch.Tensor], inv_rms_pre: Optional[torch.Tensor], dY: Optional[torch.Tensor],
+                        dN: Optional[torch.Tensor], dX: Optional[torch.Tensor], dZ: Optional[torch.Tensor], dgate: Optional[torch.Tensor] = None,
+                        dgamma_post: Optional[torch.Tensor] = None, dscale: Optional[torch.Tensor] = None,
+                        dgamma_pre: Optional[torch.Tensor] = None, stream=None):
+    """The gradients of sgnn_block_norm_fwd from what reaches Y (dY) and N (dN), either may be None; outputs None where not wanted."""
+    t = dY if dY is not None else dN
+    if t is None:
+        raise ValueError("dY or dN is needed")
+    rows, d = t.shape
+    p = _block_norm(d, gate, gamma_post, col_scale, gamma_pre, res_scale, 0.0, post)
+    ctx.check(lib().sgnn_block_norm_bwd(ctx._h, _m(Z, "Z"), _m(Y, "Y"), C.byref(p), _vec(inv_rms_post, rows, "inv_rms_post"),
+                                        _vec(inv_rms_pre, rows, "inv_rms_pre"), _m(dY, "dY"), _m(dN, "dN"), _m(dX, "dX"), _m(dZ, "dZ"), _m(dgate, "dgate"),
+                                        _vec(dgamma_post, d, "dgamma_post"), _vec(dscale, d, "dscale"), _vec(dgamma_pre, d, "dgamma_pre"), _stream(stream)))
 
 
 def sgnn_copy_f32(ctx: Context, src: torch.Tensor, dst: torch.Tensor, stream=None):

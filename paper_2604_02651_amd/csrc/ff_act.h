@@ -1,0 +1,62 @@
+// Activations of the feed-forward operators and their derivatives, in fp32:
+//   none z; ReLU max(z, 0); GELU z Phi(z), Phi the normal distribution function; GELU by tanh z s(2u), u = sqrt(2/pi) (z + 0.044715 z^3)
+//   (0.5 (1 + tanh u) = s(2u), s the logistic function); SiLU z s(z).
+// A NaN stays one.  Where z is infinite the formulas' own 0 * infinity stays NaN for GELU and SiLU; finite z never overflow into one.
+#pragma once
+
+#include "block_prims.h"
+#include "sgnn.h"
+
+struct ff_act_pair { float f, d; };       // act(z) and act'(z)
+
+// 1 / (1 + exp(-x)) from the exponential of -|x|, which cannot overflow
+__device__ __forceinline__ float ff_logistic(float x)
+{
+    const float e = exp_neg(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e);
+    return x >= 0.f ? r : (x < 0.f ? e * r : x);           // the last for a NaN
+}
+
+// 2 sqrt(2/pi) (z + 0.044715 z^3); beyond 12 in magnitude the logistic function of it is 0 or 1 in fp32
+__device__ __forceinline__ float ff_gelu_inner(float z)
+{
+    const float c = z != z ? z : fminf(fmaxf(z, -12.f), 12.f);
+    return 1.5957691216057308f * c * fmaf(0.044715f * c, c, 1.f);
+}
+
+template <int ACT> __device__ __forceinline__ float ff_act(float z)
+{
+    if constexpr (ACT == SGNN_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
+    else if constexpr (ACT == SGNN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    else if constexpr (ACT == SGNN_ACT_GELU_TANH) return z * ff_logistic(ff_gelu_inner(z));
+    else if constexpr (ACT == SGNN_ACT_SILU) return z * ff_logistic(z);
+    else return z;
+}
+
+template <int ACT> __device__ __forceinline__ ff_act_pair ff_act_both(float z)
+{
+    if constexpr (ACT == SGNN_ACT_RELU) return {ff_act<ACT>(z), z > 0.f ? 1.f : (z != z ? z : 0.f)};
+    else if constexpr (ACT == SGNN_ACT_GELU) {
+        const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        const float c = z != z ? z : fminf(fmaxf(z, -20.f), 20.f);       // the density is 0 in fp32 beyond
+        return {z * p, fmaf(c * 0.3989422804014327f, exp_neg(-0.5f * c * c), p)};
+    } else if constexpr (ACT == SGNN_ACT_GELU_TANH) {
+        const float s = ff_logistic(ff_gelu_inner(z));
+        const float c = z != z ? z : fminf(fmaxf(z, -12.f), 12.f);
+        return {z * s, fmaf(c * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f), s)};
+    } else if constexpr (ACT == SGNN_ACT_SILU) {
+        const float s = ff_logistic(z), c = z != z ? z : fminf(fmaxf(z, -120.f), 120.f);
+        return {z * s, s * fmaf(c, 1.f - s, 1.f)};
+    } else return {z, 1.f};
+}
+
+// f(integral_constant<int, act>) for an activation known at run time only
+template <class F> __device__ __forceinline__ void ff_with_act(int act, F f)
+{
+    switch (act) {
+    case SGNN_ACT_RELU: f(std::integral_constant<int, SGNN_ACT_RELU>()); break;
+    case SGNN_ACT_GELU: f(std::integral_constant<int, SGNN_ACT_GELU>()); break;
+    case SGNN_ACT_GELU_TANH: f(std::integral_constant<int, SGNN_ACT_GELU_TANH>()); break;
+    case SGNN_ACT_SILU: f(std::integral_constant<int, SGNN_ACT_SILU>()); break;
+    default: f(std::integral_constant<int, SGNN_ACT_NONE>()); break;
+    }
+}
