@@ -10,6 +10,11 @@
 // workgroup of 1024 threads.  Row sums are exchanges inside the wavefront, and through LDS between the wavefronts of a row.  Column sums stay in
 // registers over all rows of a group, the groups of a workgroup meet in LDS, every workgroup writes one partial sum a column and a second kernel
 // adds these in a fixed order: bit-reproducible.  N is taken from y before it is rounded for storage; statistics and sums are fp32.
+//
+// What else counts is instructions: at 16 fp32 lanes a SIMD some 80 an element are worth its bytes.  The vectors of the columns therefore stay in
+// registers over the rows of a group (at most 4096 workgroups, 1024 backward), the parts of a row behind its end are zeros throughout instead of being tested
+// for, and a gate costs an exponential and a reciprocal.  2^20 x 256 bfloat16 with a gate for every element: 1552 us with the vectors read and
+// the columns tested element by element, 575 here (4.7 TB/s, the rate of a copy 4.8); backward of 32768 x 256 fp32 57 -> 42 (4.8 TB/s).
 #include "ff.h"
 #include "ff_act.h"
 
@@ -35,72 +40,107 @@ template <int G> __device__ __forceinline__ void row_sum(float (&s)[2], float *l
 
 template <int G> constexpr int threads() { return G > 256 ? G : 256; }
 
+// n fp32 values of a vector at col, `one` where there is no vector, 0 behind its end (so that what is computed there is 0 as well)
+template <int V> __device__ __forceinline__ void vector_at(float (&v)[V], const float *p, int col, int left, float one)
+{
+    if (p) ff_load<FF_T32, V>(v, ff_mat{p, 0, 0}, 0, col, left);
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = i < left ? one : 0.f;
+}
+
+__device__ __forceinline__ float gate_of(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
+
+// the rows' gates: 1 without one; one[] is loaded by every lane of the row
+template <int T, int V> __device__ __forceinline__ float row_gate(const ff_norm &a, int64_t row)
+{
+    if (!a.gate.p || a.gate_cols != 1) return 1.f;
+    float one[V];
+    ff_load<T, V>(one, a.gate, row, 0, 1);
+    return gate_of(one[0]);
+}
+
 template <int T, int V, int CH, int G> __global__ __launch_bounds__(threads<G>()) void block_norm_fwd_kernel(ff_norm a)
 {
     constexpr int RPW = threads<G>() / G;
     __shared__ float lds[2 * (G > 64 ? G / 64 : 1)];
     const int l = threadIdx.x % G;
     const float inv_d = 1.f / (float)a.d;
-    // with G > 64 the workgroup has one row and leaves as a whole: no barrier is missed
-    const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / G;
-    if (row >= a.rows) return;
-    float x[CH][V], z[CH][V], w[CH][V], s[2] = {0.f, 0.f};
+    const bool full_gate = a.gate.p && a.gate_cols > 1;
+    float post[CH][V], pre[CH][V];            // gamma_post s, gamma_pre
 #pragma unroll
     for (int m = 0; m < CH; ++m) {
         const int col = (m * G + l) * V, left = a.d - col;
+        float g[V];
+        vector_at<V>(g, a.gamma_post, col, left, 1.f);
+        vector_at<V>(post[m], a.scale, col, left, 1.f);
+        vector_at<V>(pre[m], a.gamma_pre, col, left, 1.f);
 #pragma unroll
-        for (int i = 0; i < V; ++i) { x[m][i] = z[m][i] = 0.f; w[m][i] = 1.f; }
-        if (left <= 0) continue;
-        if (a.z.p) ff_load<T, V>(z[m], a.z, row, col, left);
-        if (a.x.p) ff_load<T, V>(x[m], a.x, row, col, left);
-        if (a.gate.p && a.gate_cols > 1) ff_load<T, V>(w[m], a.gate, row, col, left);
+        for (int i = 0; i < V; ++i) post[m][i] *= g[i];
     }
-    float w_row = 0.f;
-    if (a.gate.p && a.gate_cols == 1) {
-        float one[V];
-        ff_load<T, V>(one, a.gate, row, 0, 1);
-        w_row = ff_logistic(one[0]);
-    }
-    float ir = 1.f;
-    if (a.z.p && a.post) {
+    // rows are a workgroup's at a time: where a row has several wavefronts they reach every barrier together
+    for (int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * RPW) {
+        float x[CH][V], z[CH][V], w[CH][V], s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int m = 0; m < CH; ++m) {
+            const int col = (m * G + l) * V, left = a.d - col;
+            if (left > 0) {
+                if (a.z.p) ff_load<T, V>(z[m], a.z, row, col, left);
+                ff_load<T, V>(x[m], a.x, row, col, left);
+                if (full_gate) ff_load<T, V>(w[m], a.gate, row, col, left);
+            } else
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[m][i] = z[m][i] = w[m][i] = 0.f;
+        }
+        if (a.z.p) {
+            float ir = row_gate<T, V>(a, row);
+            if (a.post) {
+#pragma unroll
+                for (int m = 0; m < CH; ++m)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s[0] = fmaf(z[m][i], z[m][i], s[0]);
+                row_sum<G>(s, lds);
+                const float r = 1.f / sqrtf(s[0] * inv_d + a.eps);
+                if (a.ir_post && l == 0) a.ir_post[row] = r;
+                ir *= r;
+            }
+#pragma unroll
+            for (int m = 0; m < CH; ++m)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float b = z[m][i] * ir * post[m][i];
+                    if (full_gate) b *= gate_of(w[m][i]);
+                    x[m][i] = fmaf(a.alpha, x[m][i], b);
+                }
+        } else {
+#pragma unroll
+            for (int m = 0; m < CH; ++m)
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[m][i] *= a.alpha;
+        }
+        if (a.y.p) {
+#pragma unroll
+            for (int m = 0; m < CH; ++m) {
+                const int col = (m * G + l) * V, left = a.d - col;
+                if (left > 0) ff_store<T, V>(x[m], a.y, row, col, left);
+            }
+        }
+        if (!a.n.p) continue;
+        s[0] = s[1] = 0.f;
 #pragma unroll
         for (int m = 0; m < CH; ++m)
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[0] = fmaf(z[m][i], z[m][i], s[0]);
+            for (int i = 0; i < V; ++i) s[0] = fmaf(x[m][i], x[m][i], s[0]);
         row_sum<G>(s, lds);
-        ir = 1.f / sqrtf(s[0] * inv_d + a.eps);
-        if (a.ir_post && l == 0) a.ir_post[row] = ir;
-    }
-    s[0] = s[1] = 0.f;
+        const float ir = 1.f / sqrtf(s[0] * inv_d + a.eps);
+        if (a.ir_pre && l == 0) a.ir_pre[row] = ir;
 #pragma unroll
-    for (int m = 0; m < CH; ++m) {
-        const int col = (m * G + l) * V, left = a.d - col;
-        if (left <= 0) continue;
+        for (int m = 0; m < CH; ++m) {
+            const int col = (m * G + l) * V, left = a.d - col;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (i >= left) break;
-            float b = 0.f;
-            if (a.z.p) {
-                const float gate = a.gate.p ? (a.gate_cols == 1 ? w_row : ff_logistic(w[m][i])) : 1.f;
-                b = z[m][i] * ir * (a.gamma_post ? a.gamma_post[col + i] : 1.f) * (a.scale ? a.scale[col + i] : 1.f) * gate;
-            }
-            x[m][i] = fmaf(a.alpha, x[m][i], b);
-            s[0] = fmaf(x[m][i], x[m][i], s[0]);
+            for (int i = 0; i < V; ++i) x[m][i] *= ir * pre[m][i];
+            if (left > 0) ff_store<T, V>(x[m], a.n, row, col, left);
         }
-        if (a.y.p) ff_store<T, V>(x[m], a.y, row, col, left);
-    }
-    if (!a.n.p) return;
-    row_sum<G>(s, lds);
-    ir = 1.f / sqrtf(s[0] * inv_d + a.eps);
-    if (a.ir_pre && l == 0) a.ir_pre[row] = ir;
-#pragma unroll
-    for (int m = 0; m < CH; ++m) {
-        const int col = (m * G + l) * V, left = a.d - col;
-        if (left <= 0) continue;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < left) x[m][i] *= ir * (a.gamma_pre ? a.gamma_pre[col + i] : 1.f);
-        ff_store<T, V>(x[m], a.n, row, col, left);
     }
 }
 
@@ -111,19 +151,26 @@ template <int T, int V, int CH, int G> __global__ __launch_bounds__(threads<G>()
     __shared__ float red[RPW > 1 ? RPW * G * CH * V : 1];
     const int l = threadIdx.x % G, grp = threadIdx.x / G;
     const float inv_d = 1.f / (float)a.d;
-    float sg[CH][V], ss[CH][V], sp[CH][V];         // sums of v zh, t w b, dN yh
+    const bool full_gate = a.gate.p && a.gate_cols > 1;
+    float gp[CH][V], sc[CH][V], gn[CH][V];
+    float sg[CH][V], ss[CH][V], sp[CH][V];         // sums of v zh, t w zh (times gamma_post at the end), dN yh
 #pragma unroll
-    for (int m = 0; m < CH; ++m)
+    for (int m = 0; m < CH; ++m) {
+        const int col = (m * G + l) * V, left = a.d - col;
+        vector_at<V>(gp[m], a.gamma_post, col, left, 1.f);
+        vector_at<V>(sc[m], a.scale, col, left, 1.f);
+        vector_at<V>(gn[m], a.gamma_pre, col, left, 1.f);
 #pragma unroll
-        for (int i = 0; i < V; ++i) sg[m][i] = ss[m][i] = sp[m][i] = 0.f;
-    // rows are a workgroup's at a time: where a row has several wavefronts they reach every barrier together
+        for (int i = 0; i < V; ++i) ss[m][i] = sp[m][i] = 0.f;
+    }
+    // rows are a workgroup's at a time, as above
     for (int64_t row = (int64_t)blockIdx.x * RPW + grp; row < a.rows; row += (int64_t)gridDim.x * RPW) {
         float t[CH][V], n[CH][V], y[CH][V], z[CH][V], w[CH][V], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int m = 0; m < CH; ++m) {
             const int col = (m * G + l) * V, left = a.d - col;
 #pragma unroll
-            for (int i = 0; i < V; ++i) { t[m][i] = n[m][i] = y[m][i] = z[m][i] = 0.f; w[m][i] = 1.f; }
+            for (int i = 0; i < V; ++i) t[m][i] = n[m][i] = y[m][i] = z[m][i] = w[m][i] = 0.f;
             if (left <= 0) continue;
             if (a.dn.p) {
                 ff_load<T, V>(n[m], a.dn, row, col, left);
@@ -131,68 +178,60 @@ template <int T, int V, int CH, int G> __global__ __launch_bounds__(threads<G>()
             }
             if (a.dy.p) ff_load<T, V>(t[m], a.dy, row, col, left);
             if (a.z.p) ff_load<T, V>(z[m], a.z, row, col, left);
-            if (a.gate.p && a.gate_cols > 1) ff_load<T, V>(w[m], a.gate, row, col, left);
+            if (full_gate) ff_load<T, V>(w[m], a.gate, row, col, left);
         }
-        float w_row = 1.f;
-        if (a.gate.p && a.gate_cols == 1) {
-            float one[V];
-            ff_load<T, V>(one, a.gate, row, 0, 1);
-            w_row = ff_logistic(one[0]);
-        }
-        const float irp = a.dn.p ? a.in_ir_pre[row] : 0.f, irz = a.z.p && a.post ? a.in_ir_post[row] : 1.f;
         if (a.dn.p) {
+            const float irp = a.in_ir_pre[row];
 #pragma unroll
-            for (int m = 0; m < CH; ++m) {
-                const int col = (m * G + l) * V;
+            for (int m = 0; m < CH; ++m)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    if (col + i >= a.d) break;
                     y[m][i] *= irp;
                     sp[m][i] = fmaf(n[m][i], y[m][i], sp[m][i]);
-                    if (a.gamma_pre) n[m][i] *= a.gamma_pre[col + i];
+                    n[m][i] *= gn[m][i];
                     s[0] = fmaf(n[m][i], y[m][i], s[0]);
                 }
-            }
             row_sum<G>(s, lds);
             const float mean = s[0] * inv_d;
 #pragma unroll
             for (int m = 0; m < CH; ++m)
 #pragma unroll
-                for (int i = 0; i < V; ++i) t[m][i] = fmaf(irp, n[m][i] - y[m][i] * mean, t[m][i]);
+                for (int i = 0; i < V; ++i) t[m][i] = fmaf(irp, fmaf(-y[m][i], mean, n[m][i]), t[m][i]);
         }
+        if (a.dx.p) {
+#pragma unroll
+            for (int m = 0; m < CH; ++m) {
+                const int col = (m * G + l) * V, left = a.d - col;
+                float dx[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) dx[i] = a.alpha * t[m][i];
+                if (left > 0) ff_store<T, V>(dx, a.dx, row, col, left);
+            }
+        }
+        if (!a.z.p) continue;
+        const float wr = row_gate<T, V>(a, row), irz = a.post ? a.in_ir_post[row] : 1.f;
         // n and y are done with: n becomes h = v gamma_post, y the gate's gradient
         s[0] = s[1] = 0.f;
 #pragma unroll
         for (int m = 0; m < CH; ++m) {
             const int col = (m * G + l) * V, left = a.d - col;
-            if (left <= 0) continue;
-            if (a.dx.p) {
-                float dx[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) dx[i] = a.alpha * t[m][i];
-                ff_store<T, V>(dx, a.dx, row, col, left);
-            }
-            if (!a.z.p) continue;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                if (i >= left) break;
-                const float gate = a.gate.p ? (a.gate_cols == 1 ? w_row : ff_logistic(w[m][i])) : 1.f;
-                const float gp = a.gamma_post ? a.gamma_post[col + i] : 1.f, sc = a.scale ? a.scale[col + i] : 1.f;
+                const float gate = full_gate ? gate_of(w[m][i]) : wr;
                 z[m][i] *= irz;
-                const float b = z[m][i] * gp, ts = t[m][i] * sc, v = ts * gate;
-                ss[m][i] = fmaf(t[m][i] * gate, b, ss[m][i]);
-                sg[m][i] = fmaf(v, z[m][i], sg[m][i]);
-                y[m][i] = ts * b * gate * (1.f - gate);
-                n[m][i] = v * gp;
-                s[0] = fmaf(n[m][i], z[m][i], s[0]);
+                const float tg = t[m][i] * gate, g = tg * gp[m][i];
+                ss[m][i] = fmaf(tg, z[m][i], ss[m][i]);
+                n[m][i] = g * sc[m][i];
+                const float hz = n[m][i] * z[m][i];
+                s[0] += hz;
+                y[m][i] = fmaf(-gate, hz, hz);
                 s[1] += y[m][i];
             }
-            if (a.dgate.p && a.gate_cols > 1) ff_store<T, V>(y[m], a.dgate, row, col, left);
+            if (full_gate && a.dgate.p && left > 0) ff_store<T, V>(y[m], a.dgate, row, col, left);
         }
-        if (!a.z.p) continue;
-        const bool row_gate = a.dgate.p && a.gate_cols == 1;
-        if (a.post || row_gate) row_sum<G>(s, lds);
-        if (row_gate && l == 0) {
+        const bool one_gate = a.dgate.p && a.gate_cols == 1;
+        if (a.post || one_gate) row_sum<G>(s, lds);
+        if (one_gate && l == 0) {
             float one[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) one[i] = s[1];
@@ -203,13 +242,20 @@ template <int T, int V, int CH, int G> __global__ __launch_bounds__(threads<G>()
 #pragma unroll
             for (int m = 0; m < CH; ++m) {
                 const int col = (m * G + l) * V, left = a.d - col;
-                if (left <= 0) continue;
 #pragma unroll
-                for (int i = 0; i < V; ++i) n[m][i] = irz * (n[m][i] - z[m][i] * mean);
-                ff_store<T, V>(n[m], a.dz, row, col, left);
+                for (int i = 0; i < V; ++i) n[m][i] = irz * fmaf(-z[m][i], mean, n[m][i]);
+                if (left > 0) ff_store<T, V>(n[m], a.dz, row, col, left);
             }
         }
     }
+    // sums of t w zh: ds is gamma_post times them, dgamma_post s times them
+#pragma unroll
+    for (int m = 0; m < CH; ++m)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            sg[m][i] = ss[m][i] * sc[m][i];
+            ss[m][i] *= gp[m][i];
+        }
     if (!partial) return;
     auto out = [&](int q, float (&sum)[CH][V]) {
         float *o = partial + ((int64_t)blockIdx.x * 3 + q) * a.d;
@@ -260,7 +306,7 @@ __global__ __launch_bounds__(1024) void block_norm_sums_kernel(const float *__re
     }
 }
 
-constexpr int MAX_D = 16384, BWD_GROUPS = 1024;
+constexpr int MAX_D = 16384, BWD_GROUPS = 1024, FWD_GROUPS = 4096;
 
 // lanes of a row and chunks of a lane by the row's chunks: the fewest lanes that hold it, one chunk each up to a wavefront
 template <int T, int V, class F> int with_shape(int d, F f)
@@ -283,7 +329,7 @@ template <int T, int V> int launch_fwd(sgnn_ctx *ctx, const ff_norm &a, hipStrea
 {
     return with_shape<T, V>(a.d, [&](auto ch, auto g) -> int {
         constexpr int CH = decltype(ch)::value, G = decltype(g)::value, RPW = threads<G>() / G;
-        SGNN_LAUNCH(ctx, st, "block_norm_fwd_kernel", SGNN_TAG, (block_norm_fwd_kernel<T, V, CH, G>), dim3(cdiv(a.rows, RPW)), dim3(threads<G>()), 0, st, a);
+        SGNN_LAUNCH(ctx, st, "block_norm_fwd_kernel", SGNN_TAG, (block_norm_fwd_kernel<T, V, CH, G>), dim3((unsigned)std::min<int64_t>(cdiv(a.rows, RPW), FWD_GROUPS)), dim3(threads<G>()), 0, st, a);
         return SGNN_OK;
     });
 }
