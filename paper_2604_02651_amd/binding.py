@@ -536,41 +536,76 @@ def sgnn_gemm(ctx: Context, trans_a: bool, trans_b: bool, A: torch.Tensor, B: to
 
 # ---- feed-forward operators ----------------------------------------------------------------------
 
-def _m(t: Optional[torch.Tensor], name: str):
-    """A matrix of either storage type, or None."""
-    return None if t is None else C.byref(_mat(t, None, name, allow_bf16=True))
+# These calls take microseconds where a trained block answers for a few vertices: their arguments are checked and passed with as little as it takes.
+
+_DTYPES = {torch.float32: SGNN_F32, torch.bfloat16: SGNN_BF16}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _vec(t: Optional[torch.Tensor], n: int, name: str):
+def _ffn_stream(ctx: Context, stream):
+    """The stream of the call: the one given, or the current one of the context's device."""
+    if stream is None:
+        return _raw_stream(ctx.device) if _raw_stream is not None else torch.cuda.current_stream(ctx.device).cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _ffn_mat(ctx: Context, t: torch.Tensor, name: str) -> _Mat:
+    """A matrix of either storage type on the context's device."""
+    k = _DTYPES.get(t.dtype)
+    if k is None:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    if t.get_device() != ctx.device:
+        raise TypeError("%s must be a CUDA/HIP tensor on device %d" % (name, ctx.device))
+    shape = t.shape
+    if len(shape) != 2:
+        raise TypeError("%s must be 2-D" % name)
+    rows, cols = shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1 and rows > 0:
+        raise TypeError("%s must be contiguous in its last dimension" % name)
+    if rows <= 1 and ld < cols:
+        ld = cols          # of one row any stride is as good
+    return _Mat(t.data_ptr(), k, rows, cols, ld, None)
+
+
+def _m(ctx: Context, t: Optional[torch.Tensor], name: str):
+    return None if t is None else C.byref(_ffn_mat(ctx, t, name))
+
+
+def _vec(ctx: Context, t: Optional[torch.Tensor], n: int, name: str):
     if t is None:
         return None
+    if t.dtype is not torch.float32:
+        raise TypeError("%s must be torch.float32, got %s" % (name, t.dtype))
+    if t.get_device() != ctx.device:
+        raise TypeError("%s must be a CUDA/HIP tensor on device %d" % (name, ctx.device))
     if t.numel() != n:
         raise ValueError("%s must have %d elements" % (name, n))
     if not t.is_contiguous():
         raise TypeError("%s must be contiguous" % name)
-    return _ptr(t, torch.float32, name)
+    return t.data_ptr()
 
 
 def sgnn_linear_fwd(ctx: Context, X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], act: int, flags: int, Y: torch.Tensor,
                     R: Optional[torch.Tensor] = None, Z: Optional[torch.Tensor] = None, stream=None):
     """Y = act(X W + bias) + R; Z, if given, receives X W + bias for sgnn_linear_bwd.  R may be Y."""
-    ctx.check(lib().sgnn_linear_fwd(ctx._h, _m(X, "X"), _m(W, "W"), _vec(bias, W.shape[1], "bias"), act, flags, _m(R, "R"), _m(Y, "Y"), _m(Z, "Z"),
-                                    _stream(stream)))
+    ctx.check(lib().sgnn_linear_fwd(ctx._h, _m(ctx, X, "X"), _m(ctx, W, "W"), _vec(ctx, bias, W.shape[1], "bias"), act, flags, _m(ctx, R, "R"), _m(ctx, Y, "Y"), _m(ctx, Z, "Z"),
+                                    _ffn_stream(ctx, stream)))
 
 
 def sgnn_linear_bwd(ctx: Context, X: torch.Tensor, W: torch.Tensor, Z: Optional[torch.Tensor], act: int, flags: int, dY: torch.Tensor,
                     dX: Optional[torch.Tensor], dW: Optional[torch.Tensor], dbias: Optional[torch.Tensor], stream=None):
     """dZ = dY act'(Z); dX = dZ W^T, dW = X^T dZ, dbias = column sums of dZ; None where not wanted."""
-    ctx.check(lib().sgnn_linear_bwd(ctx._h, _m(X, "X"), _m(W, "W"), _m(Z, "Z"), act, flags, _m(dY, "dY"), _m(dX, "dX"), _m(dW, "dW"),
-                                    _vec(dbias, W.shape[1], "dbias"), _stream(stream)))
+    ctx.check(lib().sgnn_linear_bwd(ctx._h, _m(ctx, X, "X"), _m(ctx, W, "W"), _m(ctx, Z, "Z"), act, flags, _m(ctx, dY, "dY"), _m(ctx, dX, "dX"), _m(ctx, dW, "dW"),
+                                    _vec(ctx, dbias, W.shape[1], "dbias"), _ffn_stream(ctx, stream)))
 
 
 def sgnn_glu_fwd(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor], bu: Optional[torch.Tensor], act: int,
                  flags: int, H: torch.Tensor, G: Optional[torch.Tensor] = None, U: Optional[torch.Tensor] = None, stream=None):
     """H = act(X Wg + bg) * (X Wu + bu); G, U, if given, receive the two projections for sgnn_glu_bwd."""
     n = Wg.shape[1]
-    ctx.check(lib().sgnn_glu_fwd(ctx._h, _m(X, "X"), _m(Wg, "Wg"), _m(Wu, "Wu"), _vec(bg, n, "bg"), _vec(bu, n, "bu"), act, flags, _m(H, "H"), _m(G, "G"),
-                                 _m(U, "U"), _stream(stream)))
+    ctx.check(lib().sgnn_glu_fwd(ctx._h, _m(ctx, X, "X"), _m(ctx, Wg, "Wg"), _m(ctx, Wu, "Wu"), _vec(ctx, bg, n, "bg"), _vec(ctx, bu, n, "bu"), act, flags, _m(ctx, H, "H"), _m(ctx, G, "G"),
+                                 _m(ctx, U, "U"), _ffn_stream(ctx, stream)))
 
 
 def sgnn_glu_bwd(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, G: torch.Tensor, U: torch.Tensor, act: int, flags: int,
@@ -579,13 +614,13 @@ def sgnn_glu_bwd(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tens
     """dG = dH U act'(G), dU = dH act(G); dX = dG Wg^T + dU Wu^T, dWg = X^T dG, dWu = X^T dU and the column sums of dG, dU; None where
     not wanted."""
     n = Wg.shape[1]
-    ctx.check(lib().sgnn_glu_bwd(ctx._h, _m(X, "X"), _m(Wg, "Wg"), _m(Wu, "Wu"), _m(G, "G"), _m(U, "U"), act, flags, _m(dH, "dH"), _m(dX, "dX"),
-                                 _m(dWg, "dWg"), _m(dWu, "dWu"), _vec(dbg, n, "dbg"), _vec(dbu, n, "dbu"), _stream(stream)))
+    ctx.check(lib().sgnn_glu_bwd(ctx._h, _m(ctx, X, "X"), _m(ctx, Wg, "Wg"), _m(ctx, Wu, "Wu"), _m(ctx, G, "G"), _m(ctx, U, "U"), act, flags, _m(ctx, dH, "dH"), _m(ctx, dX, "dX"),
+                                 _m(ctx, dWg, "dWg"), _m(ctx, dWu, "dWu"), _vec(ctx, dbg, n, "dbg"), _vec(ctx, dbu, n, "dbu"), _ffn_stream(ctx, stream)))
 
 
-def _block_norm(d: int, gate, gamma_post, col_scale, gamma_pre, res_scale: float, eps: float, post: bool) -> _BlockNorm:
-    g = C.pointer(_mat(gate, None, "gate", allow_bf16=True)) if gate is not None else None
-    return _BlockNorm(g, _vec(gamma_post, d, "gamma_post"), _vec(col_scale, d, "col_scale"), _vec(gamma_pre, d, "gamma_pre"), res_scale, eps, int(post))
+def _block_norm(ctx: Context, d: int, gate, gamma_post, col_scale, gamma_pre, res_scale: float, eps: float, post: bool) -> _BlockNorm:
+    g = C.pointer(_ffn_mat(ctx, gate, "gate")) if gate is not None else None
+    return _BlockNorm(g, _vec(ctx, gamma_post, d, "gamma_post"), _vec(ctx, col_scale, d, "col_scale"), _vec(ctx, gamma_pre, d, "gamma_pre"), res_scale, eps, int(post))
 
 
 def sgnn_block_norm_fwd(ctx: Context, X: torch.Tensor, Z: Optional[torch.Tensor], gate: Optional[torch.Tensor], gamma_post: Optional[torch.Tensor],
@@ -594,9 +629,9 @@ def sgnn_block_norm_fwd(ctx: Context, X: torch.Tensor, Z: Optional[torch.Tensor]
                         inv_rms_pre: Optional[torch.Tensor] = None, stream=None):
     """Y = res_scale X + col_scale sigmoid(gate) b, b = gamma_post rmsnorm(Z) (post) or Z; N = gamma_pre rmsnorm(Y).  gate: a matrix like Z or one
     column.  inv_rms_*: kept for sgnn_block_norm_bwd.  Y may be X."""
-    p = _block_norm(X.shape[1], gate, gamma_post, col_scale, gamma_pre, res_scale, eps, post)
-    ctx.check(lib().sgnn_block_norm_fwd(ctx._h, _m(X, "X"), _m(Z, "Z"), C.byref(p), _m(Y, "Y"), _m(N, "N"), _vec(inv_rms_post, X.shape[0], "inv_rms_post"),
-                                        _vec(inv_rms_pre, X.shape[0], "inv_rms_pre"), _stream(stream)))
+    p = _block_norm(ctx, X.shape[1], gate, gamma_post, col_scale, gamma_pre, res_scale, eps, post)
+    ctx.check(lib().sgnn_block_norm_fwd(ctx._h, _m(ctx, X, "X"), _m(ctx, Z, "Z"), C.byref(p), _m(ctx, Y, "Y"), _m(ctx, N, "N"), _vec(ctx, inv_rms_post, X.shape[0], "inv_rms_post"),
+                                        _vec(ctx, inv_rms_pre, X.shape[0], "inv_rms_pre"), _ffn_stream(ctx, stream)))
 
 
 def sgnn_block_norm_bwd(ctx: Context, Z: Optional[torch.Tensor], Y: Optional[torch.Tensor], gate: Optional[torch.Tensor],
@@ -610,10 +645,10 @@ def sgnn_block_norm_bwd(ctx: Context, Z: Optional[torch.Tensor], Y: Optional[tor
     if t is None:
         raise ValueError("dY or dN is needed")
     rows, d = t.shape
-    p = _block_norm(d, gate, gamma_post, col_scale, gamma_pre, res_scale, 0.0, post)
-    ctx.check(lib().sgnn_block_norm_bwd(ctx._h, _m(Z, "Z"), _m(Y, "Y"), C.byref(p), _vec(inv_rms_post, rows, "inv_rms_post"),
-                                        _vec(inv_rms_pre, rows, "inv_rms_pre"), _m(dY, "dY"), _m(dN, "dN"), _m(dX, "dX"), _m(dZ, "dZ"), _m(dgate, "dgate"),
-                                        _vec(dgamma_post, d, "dgamma_post"), _vec(dscale, d, "dscale"), _vec(dgamma_pre, d, "dgamma_pre"), _stream(stream)))
+    p = _block_norm(ctx, d, gate, gamma_post, col_scale, gamma_pre, res_scale, 0.0, post)
+    ctx.check(lib().sgnn_block_norm_bwd(ctx._h, _m(ctx, Z, "Z"), _m(ctx, Y, "Y"), C.byref(p), _vec(ctx, inv_rms_post, rows, "inv_rms_post"),
+                                        _vec(ctx, inv_rms_pre, rows, "inv_rms_pre"), _m(ctx, dY, "dY"), _m(ctx, dN, "dN"), _m(ctx, dX, "dX"), _m(ctx, dZ, "dZ"), _m(ctx, dgate, "dgate"),
+                                        _vec(ctx, dgamma_post, d, "dgamma_post"), _vec(ctx, dscale, d, "dscale"), _vec(ctx, dgamma_pre, d, "dgamma_pre"), _ffn_stream(ctx, stream)))
 
 
 def sgnn_copy_f32(ctx: Context, src: torch.Tensor, dst: torch.Tensor, stream=None):

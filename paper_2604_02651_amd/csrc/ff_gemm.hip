@@ -280,8 +280,8 @@ template <int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR
     const uint64_t tiles = (uint64_t)a.mtiles * a.ntiles * a.mats * a.splits;
     if (tiles > 0x70000000ull || slices > 0x7fffffff) return sgnn_fail(ctx, SGNN_ERR_UNSUPPORTED, "feed-forward product: more than 2^31 tiles");
     SGNN_HIP(ctx, (sgnn_allow_lds<&ff_gemm_kernel<BM, BN, WM, WN, BK, STAGES, ATR, BTR, KIND>>(ctx, LDS)));
-    char tag[56];
-    snprintf(tag, sizeof(tag), "%c%c%s %dx%d %lldx%dx%lld", ATR ? 'T' : 'N', BTR ? 'N' : 'T', KIND == FFK_GLU ? " gated" : "", BM, BN, (long long)a.M, a.N, (long long)a.K);
+    char tag[56] = "";
+    if (ctx->prof_on) snprintf(tag, sizeof(tag), "%c%c%s %dx%d %lldx%dx%lld", ATR ? 'T' : 'N', BTR ? 'N' : 'T', KIND == FFK_GLU ? " gated" : "", BM, BN, (long long)a.M, a.N, (long long)a.K);
     SGNN_LAUNCH(ctx, st, "ff_gemm_kernel", tag, (ff_gemm_kernel<BM, BN, WM, WN, BK, STAGES, ATR, BTR, KIND>), dim3((unsigned)((tiles + 7) / 8 * 8)),
                 dim3(64 * WM * WN), LDS, st, a);
     return SGNN_OK;
