@@ -39,11 +39,15 @@ struct sgnn_ctx {
 #define SGNN_PERSIST_STATUS_OFF (32768 - 256)
 #define SGNN_PERSIST_XENT_OFF 32768
 #define SGNN_PERSIST_XENT_BYTES (256 * 513 * 8)
-#define SGNN_PERSIST_BYTES (SGNN_PERSIST_XENT_OFF + SGNN_PERSIST_XENT_BYTES)
+// Behind those one count of arrivals for each column strip of a feed-forward product of few rows (zero between calls).
+#define SGNN_PERSIST_FFN_OFF (SGNN_PERSIST_XENT_OFF + SGNN_PERSIST_XENT_BYTES)
+#define SGNN_PERSIST_FFN_BYTES (256 * 4)
+#define SGNN_PERSIST_BYTES (SGNN_PERSIST_FFN_OFF + SGNN_PERSIST_FFN_BYTES)
 
 // Areas of the persistent memory that are zero between calls: a call adds to them in one kernel and a later one of its kernels leaves zeros.
 #define SGNN_ZERO_XENT 1u
 #define SGNN_ZERO_SAMPLER 2u
+#define SGNN_ZERO_FFN 4u
 
 // status bits
 #define SGNN_ST_CAND_OVERFLOW 1u

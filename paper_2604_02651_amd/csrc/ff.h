@@ -107,6 +107,13 @@ int sgnn_launch_ff_tn(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int mats, 
                       ws_alloc *ws, hipStream_t st);
 size_t sgnn_ff_tn_ws_bytes(uint64_t rows, uint64_t d_in, uint64_t d_out);
 
+// ---- ff_rows.hip: the same for a few rows, matrices as they come ----------------------------------
+// nn: weights [K x N] (two: gated); else nt over segs segments.  SGNN_ERR_UNSUPPORTED (nothing launched) for projections stored differently
+int sgnn_launch_ff_rows(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int segs, int mats, bool nn, bool b16, const ff_mat *X, const ff_mat *W, const ff_epilogue &e,
+                        ws_alloc *ws, hipStream_t st);
+int64_t sgnn_ff_rows_max(int64_t N, int64_t K);
+size_t sgnn_ff_rows_ws_bytes();
+
 // ---- ff_elem.hip --------------------------------------------------------------------------------
 // dst [rows x ff_pad8(cols)] = src in bfloat16, zeros behind the last column
 int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, u16 *dst, int64_t ldd, hipStream_t st);

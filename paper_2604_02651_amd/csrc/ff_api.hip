@@ -92,8 +92,21 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
     if (rc) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
     ws_alloc ws(ctx);
-    if (flags & SGNN_BF16_MFMA) {
-        ff_epilogue e = {};
+    const bool b16 = (flags & SGNN_BF16_MFMA) != 0;
+    ff_epilogue e = {};
+    for (int q = 0; q < n; ++q) {
+        e.bias[q] = b[q];
+        e.Z[q] = view(Z[q]);
+    }
+    e.act = act;
+    e.R = view(R);
+    e.Y = view(Y);
+    if (M <= sgnn_ff_rows_max(N, K)) {
+        const ff_mat x = view(X), wv[2] = {view(W[0]), view(W[n - 1])};
+        rc = sgnn_launch_ff_rows(ctx, M, N, K, 1, n, true, b16, &x, wv, e, &ws, st);
+        if (rc != SGNN_ERR_UNSUPPORTED) return rc;
+    }
+    if (b16) {
         const u16 *a, *w[2];
         int64_t lda, ldw[2];
         rc = operand(ctx, name, X, &ws, st, &a, &lda);
@@ -101,12 +114,7 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
         for (int q = 0; q < n; ++q) {
             rc = operand(ctx, name, W[q], &ws, st, &w[q], &ldw[q]);
             if (rc) return rc;
-            e.bias[q] = b[q];
-            e.Z[q] = view(Z[q]);
         }
-        e.act = act;
-        e.R = view(R);
-        e.Y = view(Y);
         return n == 1 ? sgnn_launch_ff_linear(ctx, M, N, K, a, lda, w[0], ldw[0], e, st) : sgnn_launch_ff_glu(ctx, M, N, K, a, lda, w[0], ldw[0], w[1], ldw[1], e, st);
     }
     // fp32: the library's split products, then the activation
@@ -161,6 +169,18 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     const ff_mat z0 = need_z ? view(Z[0]) : view(dY), z1 = n == 2 ? view(Z[1]) : ff_mat{};
     rc = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, n == 2 ? &z1 : nullptr, d0, n == 2 ? &d1 : nullptr, db, &ws, st);
     if (rc) return rc;
+    // the gradient of a few rows; dX, if it is still wanted, by the tile kernels
+    auto few_rows = [&]() -> int {
+        if (!dX || M > sgnn_ff_rows_max(K, n * N)) return SGNN_ERR_UNSUPPORTED;
+        ff_epilogue e = {};
+        e.Y = view(dX);
+        const ff_mat x[2] = {d0, n == 2 ? d1 : d0}, wv[2] = {view(W[0]), view(W[n - 1])};
+        return sgnn_launch_ff_rows(ctx, M, K, N, n, 1, false, b16, x, wv, e, &ws, st);
+    };
+    rc = few_rows();
+    if (rc != SGNN_OK && rc != SGNN_ERR_UNSUPPORTED) return rc;
+    if (rc == SGNN_OK) dX = nullptr;
+    rc = SGNN_OK;
     if (b16) {
         const u16 *dp[2] = {static_cast<const u16 *>(d0.p), static_cast<const u16 *>(d1.p)};
         if (any_dw) {
@@ -236,7 +256,7 @@ int sgnn_ctx_reserve_ffn(sgnn_ctx *ctx, uint64_t rows, uint32_t d_in, uint32_t d
     const uint64_t di = ff_pad8(d_in), dn = ff_pad8(d_out);
     // fp32 split products: at most 256 ranges of the reduction, and 2304 tiles of 256 x 128 over all ranges
     const uint64_t split = std::min<uint64_t>(2304ull * 256 * 128 * 4, d_in >= 4096 || d_out >= 4096 ? ~0ull : 257 * 4 * di * dn) + 257 * 4 * std::max(di, dn);
-    size_t need = rows * (2 * dn * 4 + di * 2) + 2 * di * dn * 4 * 2 + split + sgnn_ff_tn_ws_bytes(rows, di, dn) + sgnn_ff_sums_ws_bytes(dn) + 16 * 256;
+    size_t need = rows * (2 * dn * 4 + di * 2) + 2 * di * dn * 4 * 2 + split + sgnn_ff_tn_ws_bytes(rows, di, dn) + sgnn_ff_sums_ws_bytes(dn) + sgnn_ff_rows_ws_bytes() + 16 * 256;
     need = std::max(need, sgnn_block_norm_ws_bytes(std::max(d_in, d_out)));
     if (need > ctx->ws_bytes) {
         SGNN_HIP(ctx, hipDeviceSynchronize());
