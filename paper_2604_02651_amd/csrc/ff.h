@@ -16,7 +16,7 @@ __device__ __forceinline__ float ff_lo(uint32_t w) { return __builtin_bit_cast(f
 __device__ __forceinline__ float ff_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
 
 // an operand's eight values from LDS; __restrict__ for the reason given at read_tr
-__device__ __forceinline__ bf16x8 read_row(const unsigned char *__restrict__ p) { return *reinterpret_cast<const bf16x8 *>(p); }
+__device__ __forceinline__ u32x4 read_row(const unsigned char *__restrict__ p) { return *reinterpret_cast<const u32x4 *>(p); }
 
 // storage of a matrix: known when the kernel is compiled, or a field of its arguments
 enum { FF_T32 = 0, FF_T16 = 1, FF_TANY = 2 };
@@ -87,25 +87,35 @@ static inline bool ff_chunked(const void *p, int64_t cols, int64_t ld)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && cols % 8 == 0 && ld % 8 == 0 && ld <= (1 << 22);
 }
 
-// ---- ff_gemm.hip: products of bfloat16 matrices -------------------------------------------------
+// The context's words of these products: zero between calls (but for the exponents)
+struct ff_words { uint32_t *arrived, *key, *largest; int32_t *ex; };
+static inline ff_words sgnn_ff_words(sgnn_ctx *ctx)
+{
+    uint32_t *p = reinterpret_cast<uint32_t *>(ctx->persist + SGNN_PERSIST_FFN_OFF);
+    return {p, p + SGNN_FFN_COUNTS, p + SGNN_FFN_COUNTS + 1, reinterpret_cast<int32_t *>(p + SGNN_FFN_COUNTS + 4)};
+}
+static inline int sgnn_ff_open(sgnn_ctx *ctx, hipStream_t st) { return sgnn_zero_open(ctx, SGNN_ZERO_FFN, ctx->persist + SGNN_PERSIST_FFN_OFF, SGNN_PERSIST_FFN_BYTES, st); }
+static inline int sgnn_ff_close(sgnn_ctx *ctx, int rc, hipStream_t st) { return sgnn_zero_close(ctx, rc, SGNN_ZERO_FFN, ctx->persist + SGNN_PERSIST_FFN_OFF, SGNN_PERSIST_FFN_BYTES, st); }
+
+// ---- ff_gemm.hip: products of any size ----------------------------------------------------------
 struct ff_epilogue {
     int act;                          // SGNN_ACT_*
     const float *bias[2];             // of each projection, or null
     ff_mat R, Y, Z[2];                // residual, result, pre-activations kept (p may be null but for Y)
 };
-// Y = act(A B + bias) + R; A [M x K], B [K x N].  All matrices chunked (ff_chunked), the epilogue's as they come
-int sgnn_launch_ff_linear(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const u16 *A, int64_t lda, const u16 *B, int64_t ldb, const ff_epilogue &e,
-                          hipStream_t st);
-// Y = act(A B0 + bias0) * (A B1 + bias1)
-int sgnn_launch_ff_glu(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const u16 *A, int64_t lda, const u16 *B0, int64_t ldb0, const u16 *B1, int64_t ldb1,
-                       const ff_epilogue &e, hipStream_t st);
-// Y = sum over s < segs of A[s] B[s]^T; A[s] [M x K], B[s] [N x K]
-int sgnn_launch_ff_nt(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int segs, const u16 *const *A, int64_t lda, const u16 *const *B, int64_t ldb,
-                      const ff_mat &Y, hipStream_t st);
-// C[s] = A^T B[s] for s < mats; A [K x M], B[s] [K x N]
-int sgnn_launch_ff_tn(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int mats, const u16 *A, int64_t lda, const u16 *const *B, int64_t ldb, const ff_mat *C,
-                      ws_alloc *ws, hipStream_t st);
-size_t sgnn_ff_tn_ws_bytes(uint64_t rows, uint64_t d_in, uint64_t d_out);
+// an operand, chunked (ff_chunked): bfloat16 (pl = 1), or two planes of fp16 parts `plane` elements apart (pl = 2: fp32).  ex_rows, ex: the scales of the
+// rows of A, if they have their own, and of everything else (of both operands together)
+struct ff_op { const u16 *p; int64_t ld, plane; };
+// Y = act(A B + bias) + R, with mats = 2 Y = act(A B0 + bias0) * (A B1 + bias1); A [M x K], B [K x N]; the epilogue's matrices as they come
+int sgnn_launch_ff_nn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
+                      const ff_epilogue &e, ws_alloc *ws, hipStream_t st);
+// Y = sum over s < segs of A[s] B[s]^T; A[s] [M x K], B[s] [N x K], laid out alike
+int sgnn_launch_ff_nt(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int segs, const ff_op *A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
+                      const ff_mat &Y, ws_alloc *ws, hipStream_t st);
+// C[s] = A^T B[s] for s < mats; A [K x M], B[s] [K x N], laid out alike
+int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
+                      const ff_mat *C, ws_alloc *ws, hipStream_t st);
+size_t sgnn_ff_gemm_ws_bytes(uint64_t d_in, uint64_t d_out);
 
 // ---- ff_rows.hip: the same for a few rows, matrices as they come ----------------------------------
 // nn: weights [K x N] (two: gated); else nt over segs segments.  SGNN_ERR_UNSUPPORTED (nothing launched) for projections stored differently
@@ -117,10 +127,18 @@ size_t sgnn_ff_rows_ws_bytes();
 // ---- ff_elem.hip --------------------------------------------------------------------------------
 // dst [rows x ff_pad8(cols)] = src in bfloat16, zeros behind the last column
 int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, u16 *dst, int64_t ldd, hipStream_t st);
-// fp32 copy of a matrix, zeros in the columns from cols to pcols
-int sgnn_launch_ff_copy32(sgnn_ctx *ctx, const float *src, int64_t lds_, int64_t rows, int64_t cols, int64_t pcols, float *dst, int64_t ldd, hipStream_t st);
-// fp32: Y = act(Z0) + R, or with Z1 Y = act(Z0) * Z1
-int sgnn_launch_ff_apply(sgnn_ctx *ctx, int64_t rows, int64_t cols, int act, const ff_mat &Z0, const ff_mat *Z1, const ff_mat &R, const ff_mat &Y, hipStream_t st);
+// fp32 operands as two planes of fp16 parts [rows x ff_pad8(cols)], zeros behind the last column (ff_gemm.hip says how and why).
+struct ff_scan { const float *p; int64_t rows, cols, ld; };
+// The rows of one matrix, each scaled by a power of two of its own: 2^ex[row] takes the row's largest finite magnitude to [2^14, 2^15); FF_EX_ZERO
+// for a row without one.  to null: the exponents only.  With `other`, the exponents of another matrix' rows, *key = max(*key, FF_EX_KEY - ex[row] -
+// other[row]).  The same launch finds the largest finite magnitude of up to two weight matrices, *word = max(*word, its bits).
+struct ff_row_parts { ff_scan m; u16 *to; int64_t ld, plane; int32_t *ex; const int32_t *other; uint32_t *key; };
+constexpr int FF_EX_ZERO = 2000, FF_EX_KEY = 8192;
+int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *word, hipStream_t st);
+// Up to three matrices with the scale known: rows == null, one for the matrix, from the largest magnitude in *word; else FF_EX_KEY - *word - rows[row] for
+// each row.  *ex: the scale of the matrix, or FF_EX_KEY - *word
+struct ff_parts { ff_scan m; const uint32_t *word; const int32_t *rows; int32_t *ex; u16 *to; int64_t ld, plane; };
+int sgnn_launch_ff_parts(sgnn_ctx *ctx, int n, const ff_parts *m, hipStream_t st);
 // D0 = dY * act'(Z0), or with Z1 D0 = dY * Z1 * act'(Z0) and D1 = dY * act(Z0); zeros in the columns from cols to pcols; column sums (before
 // the rounding) to db[0], db[1] where they are wanted
 int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pcols, int act, const ff_mat &dY, const ff_mat &Z0, const ff_mat *Z1,

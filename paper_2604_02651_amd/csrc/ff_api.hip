@@ -33,23 +33,28 @@ int bind(sgnn_ctx *ctx)
 
 int no_scratch(sgnn_ctx *ctx, const char *name) { return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "%s: scratch too small: call sgnn_ctx_reserve_ffn", name); }
 
-// m as an operand of the tile kernel: as it lies, or packed into scratch
-int operand(sgnn_ctx *ctx, const char *name, const sgnn_mat *m, ws_alloc *ws, hipStream_t st, const u16 **p, int64_t *ld)
+// m as a bfloat16 operand of the tile kernels: as it lies, or packed into scratch (always with `pack`)
+int operand(sgnn_ctx *ctx, const char *name, const sgnn_mat *m, bool pack, ws_alloc *ws, hipStream_t st, ff_op *op)
 {
-    if (m->dtype == SGNN_BF16 && ff_chunked(m->ptr, m->cols, m->ld)) {
-        *p = static_cast<const u16 *>(m->ptr);
-        *ld = m->ld;
+    if (!pack && m->dtype == SGNN_BF16 && ff_chunked(m->ptr, m->cols, m->ld)) {
+        *op = ff_op{static_cast<const u16 *>(m->ptr), m->ld, 0};
         return SGNN_OK;
     }
-    *ld = ff_pad8(m->cols);
-    u16 *to = ws->get<u16>((size_t)m->rows * *ld);
+    const int64_t ld = ff_pad8(m->cols);
+    u16 *to = ws->get<u16>((size_t)m->rows * ld);
     if (!ws->ok) return no_scratch(ctx, name);
-    *p = to;
-    return sgnn_launch_ff_pack(ctx, view(m), m->rows, m->cols, to, *ld, st);
+    *op = ff_op{to, ld, 0};
+    return sgnn_launch_ff_pack(ctx, view(m), m->rows, m->cols, to, ld, st);
 }
 
-const float *f32(const sgnn_mat *m) { return static_cast<const float *>(m->ptr); }
-float *f32_out(const sgnn_mat *m) { return static_cast<float *>(m->ptr); }
+ff_scan scan(const sgnn_mat *m) { return ff_scan{static_cast<const float *>(m->ptr), m->rows, m->cols, m->ld}; }
+
+// scratch for the parts of an fp32 matrix
+ff_op parts_op(ws_alloc *ws, int64_t rows, int64_t cols)
+{
+    const int64_t ld = ff_pad8(cols);
+    return ff_op{ws->get<u16>((size_t)2 * rows * ld), ld, rows * ld};
+}
 
 // zeros for the gradients of weights and biases of a batch without rows
 int no_rows(sgnn_ctx *ctx, int n, sgnn_mat *const *dW, float *const *db, int64_t cols, hipStream_t st)
@@ -102,36 +107,37 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
     e.R = view(R);
     e.Y = view(Y);
     if (M <= sgnn_ff_rows_max(N, K)) {
-        const ff_mat x = view(X), wv[2] = {view(W[0]), view(W[n - 1])};
-        rc = sgnn_launch_ff_rows(ctx, M, N, K, 1, n, true, b16, &x, wv, e, &ws, st);
+        const ff_mat xv = view(X), wv[2] = {view(W[0]), view(W[n - 1])};
+        rc = sgnn_launch_ff_rows(ctx, M, N, K, 1, n, true, b16, &xv, wv, e, &ws, st);
         if (rc != SGNN_ERR_UNSUPPORTED) return rc;
     }
+    ff_op x, w[2];
     if (b16) {
-        const u16 *a, *w[2];
-        int64_t lda, ldw[2];
-        rc = operand(ctx, name, X, &ws, st, &a, &lda);
+        rc = operand(ctx, name, X, false, &ws, st, &x);
+        for (int q = 0; q < n && !rc; ++q) rc = operand(ctx, name, W[q], false, &ws, st, &w[q]);
         if (rc) return rc;
-        for (int q = 0; q < n; ++q) {
-            rc = operand(ctx, name, W[q], &ws, st, &w[q], &ldw[q]);
-            if (rc) return rc;
-        }
-        return n == 1 ? sgnn_launch_ff_linear(ctx, M, N, K, a, lda, w[0], ldw[0], e, st) : sgnn_launch_ff_glu(ctx, M, N, K, a, lda, w[0], ldw[0], w[1], ldw[1], e, st);
+        return sgnn_launch_ff_nn(ctx, 1, M, N, K, n, x, w, nullptr, nullptr, e, &ws, st);
     }
-    // fp32: the library's split products, then the activation
-    ff_mat z[2];
+    const ff_words words = sgnn_ff_words(ctx);
+    ff_scan ws_[2];
+    ff_parts wp[2];
+    x = parts_op(&ws, M, K);
+    int32_t *const ex_rows = ws.get<int32_t>((size_t)M);
     for (int q = 0; q < n; ++q) {
-        if (Z[q]) z[q] = view(Z[q]);
-        else if (q == 1) z[q] = view(Y);          // read and written by the same thread
-        else {
-            float *p = ws.get<float>((size_t)M * ff_pad8(N));
-            if (!ws.ok) return no_scratch(ctx, name);
-            z[q] = ff_mat{p, ff_pad8(N), 0};
-        }
-        rc = sgnn_launch_gemm(ctx, 0, 0, M, N, K, f32(X), X->ld, nullptr, f32(W[q]), W[q]->ld, b[q], 0, static_cast<float *>(const_cast<void *>(z[q].p)), z[q].ld,
-                              nullptr, 0, nullptr, &ws, st);
-        if (rc) return rc;
+        w[q] = parts_op(&ws, K, N);
+        ws_[q] = scan(W[q]);
+        wp[q] = ff_parts{ws_[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld, w[q].plane};
     }
-    return sgnn_launch_ff_apply(ctx, M, N, act, z[0], n == 2 ? &z[1] : nullptr, view(R), view(Y), st);
+    if (!ws.ok) return no_scratch(ctx, name);
+    rc = sgnn_ff_open(ctx, st);
+    if (rc) return rc;
+    auto run = [&]() -> int {
+        const ff_row_parts xr = {scan(X), const_cast<u16 *>(x.p), x.ld, x.plane, ex_rows, nullptr, nullptr};
+        int r = sgnn_launch_ff_row_parts(ctx, xr, n, ws_, words.largest, st);
+        if (!r) r = sgnn_launch_ff_parts(ctx, n, wp, st);
+        return r ? r : sgnn_launch_ff_nn(ctx, 2, M, N, K, n, x, w, ex_rows, words.ex, e, &ws, st);
+    };
+    return sgnn_ff_close(ctx, run(), st);
 }
 
 // Backward of either: D = the gradients of the pre-activations, then the products
@@ -167,80 +173,92 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     if (!ws.ok) return no_scratch(ctx, name);
     const ff_mat d0 = {D, ldd, b16}, d1 = {b16 ? static_cast<void *>(static_cast<u16 *>(D) + np) : static_cast<void *>(static_cast<float *>(D) + np), ldd, b16};
     const ff_mat z0 = need_z ? view(Z[0]) : view(dY), z1 = n == 2 ? view(Z[1]) : ff_mat{};
-    rc = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, n == 2 ? &z1 : nullptr, d0, n == 2 ? &d1 : nullptr, db, &ws, st);
-    if (rc) return rc;
-    // the gradient of a few rows; dX, if it is still wanted, by the tile kernels
+    const ff_mat *zp = n == 2 ? &z1 : nullptr, *dp = n == 2 ? &d1 : nullptr;
+    const bool few = dX && M <= sgnn_ff_rows_max(K, n * N);
+    // the gradient of a few rows
     auto few_rows = [&]() -> int {
-        if (!dX || M > sgnn_ff_rows_max(K, n * N)) return SGNN_ERR_UNSUPPORTED;
         ff_epilogue e = {};
         e.Y = view(dX);
-        const ff_mat x[2] = {d0, n == 2 ? d1 : d0}, wv[2] = {view(W[0]), view(W[n - 1])};
-        return sgnn_launch_ff_rows(ctx, M, K, N, n, 1, false, b16, x, wv, e, &ws, st);
+        const ff_mat xv[2] = {d0, n == 2 ? d1 : d0}, wv[2] = {view(W[0]), view(W[n - 1])};
+        return sgnn_launch_ff_rows(ctx, M, K, N, n, 1, false, b16, xv, wv, e, &ws, st);
     };
-    rc = few_rows();
-    if (rc != SGNN_OK && rc != SGNN_ERR_UNSUPPORTED) return rc;
-    if (rc == SGNN_OK) dX = nullptr;
-    rc = SGNN_OK;
+    // both weight gradients in one launch, or the one that is wanted
+    auto weights = [&](int pl, const ff_op &x, const ff_op *d, const int32_t *ex_x, const int32_t *ex_d) -> int {
+        ff_op b[2];
+        ff_mat c[2];
+        int mats = 0;
+        for (int q = 0; q < n; ++q)
+            if (dW[q]) { b[mats] = d[q]; c[mats++] = view(dW[q]); }
+        return sgnn_launch_ff_tn(ctx, pl, K, N, M, mats, x, b, ex_x, ex_d, c, &ws, st);
+    };
+    ff_op x, w[2];
     if (b16) {
-        const u16 *dp[2] = {static_cast<const u16 *>(d0.p), static_cast<const u16 *>(d1.p)};
+        rc = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, zp, d0, dp, db, &ws, st);
+        if (rc) return rc;
+        bool dx_done = false;
+        if (few) {
+            rc = few_rows();
+            if (rc != SGNN_OK && rc != SGNN_ERR_UNSUPPORTED) return rc;
+            dx_done = rc == SGNN_OK;
+        }
+        const ff_op d[2] = {{static_cast<const u16 *>(d0.p), ldd, 0}, {static_cast<const u16 *>(d1.p), ldd, 0}};
         if (any_dw) {
             const size_t off = ws.off;
-            const u16 *a;
-            int64_t lda;
-            rc = operand(ctx, name, X, &ws, st, &a, &lda);
+            rc = operand(ctx, name, X, false, &ws, st, &x);
             if (rc) return rc;
-            // both results of one launch, or the one that is wanted
-            const u16 *bp[2];
-            ff_mat c[2];
-            int mats = 0;
-            for (int q = 0; q < n; ++q)
-                if (dW[q]) { bp[mats] = dp[q]; c[mats++] = view(dW[q]); }
-            rc = sgnn_launch_ff_tn(ctx, K, N, M, mats, a, lda, bp, ldd, c, &ws, st);
+            rc = weights(1, x, d, nullptr, nullptr);
             if (rc) return rc;
             ws.off = off;
         }
-        if (dX) {
-            const u16 *w[2];
-            int64_t ldw[2];
-            for (int q = 0; q < n; ++q) {
-                rc = operand(ctx, name, W[q], &ws, st, &w[q], &ldw[q]);
-                if (rc) return rc;
-            }
-            if (n == 2 && ldw[0] != ldw[1]) {       // one leading dimension for both
-                for (int q = 0; q < 2; ++q) {
-                    u16 *to = ws.get<u16>((size_t)K * np);
-                    if (!ws.ok) return no_scratch(ctx, name);
-                    rc = sgnn_launch_ff_pack(ctx, view(W[q]), K, N, to, np, st);
-                    if (rc) return rc;
-                    w[q] = to;
-                    ldw[q] = np;
-                }
-            }
-            rc = sgnn_launch_ff_nt(ctx, M, K, N, n, dp, ldd, w, ldw[0], view(dX), st);
-        }
-        return rc;
-    }
-    for (int q = 0; q < n; ++q)
-        if (dW[q]) {
-            rc = sgnn_launch_gemm(ctx, 1, 0, K, N, M, f32(X), X->ld, nullptr, static_cast<const float *>(q ? d1.p : d0.p), ldd, nullptr, 0, f32_out(dW[q]), dW[q]->ld,
-                                  nullptr, 0, nullptr, &ws, st);
+        if (!dX || dx_done) return SGNN_OK;
+        // two projections laid out alike, by packing both if they are not
+        const bool pack = n == 2 && (W[0]->ld != W[1]->ld || is16(W[0]) != is16(W[1]) || ff_chunked(W[0]->ptr, N, W[0]->ld) != ff_chunked(W[1]->ptr, N, W[1]->ld));
+        for (int q = 0; q < n; ++q) {
+            rc = operand(ctx, name, W[q], pack, &ws, st, &w[q]);
             if (rc) return rc;
         }
-    if (!dX) return SGNN_OK;
-    const float *w = f32(W[0]);
-    int64_t ldw = W[0]->ld, kk = N;
-    if (n == 2) {
-        // [W0 | W1], so that the sum over both is one product
-        float *to = ws.get<float>((size_t)K * ldd);
+        return sgnn_launch_ff_nt(ctx, 1, M, K, N, n, d, w, nullptr, nullptr, view(dX), &ws, st);
+    }
+    // fp32: the gradients' rows are scaled by themselves, the rows of X so that with the gradients' all products have one scale (ff_gemm.hip)
+    const bool tiles_dx = dX && !few, split = any_dw || tiles_dx;
+    const ff_words words = sgnn_ff_words(ctx);
+    ff_op d[2];
+    ff_parts job[3];
+    ff_scan wscan[2];
+    int jobs = 0, nw = 0;
+    int32_t *ex_x = nullptr, *ex_d = nullptr;
+    if (split) {
+        if (any_dw) {
+            x = parts_op(&ws, M, K);
+            ex_x = ws.get<int32_t>((size_t)M);
+        }
+        d[0] = d[1] = parts_op(&ws, M, ldd);
+        d[1].p += np;
+        ex_d = ws.get<int32_t>((size_t)M);
+        if (any_dw) job[jobs++] = ff_parts{scan(X), words.key, ex_d, words.ex + 1, const_cast<u16 *>(x.p), x.ld, x.plane};
+        for (int q = 0; q < n && tiles_dx; ++q) {
+            w[q] = parts_op(&ws, K, N);
+            wscan[nw++] = scan(W[q]);
+            job[jobs++] = ff_parts{wscan[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld, w[q].plane};
+        }
         if (!ws.ok) return no_scratch(ctx, name);
-        for (int q = 0; q < 2; ++q) {
-            rc = sgnn_launch_ff_copy32(ctx, f32(W[q]), W[q]->ld, K, N, np, to + q * np, ldd, st);
-            if (rc) return rc;
-        }
-        w = to;
-        ldw = kk = ldd;
+        rc = sgnn_ff_open(ctx, st);
+        if (rc) return rc;
     }
-    return sgnn_launch_gemm(ctx, 0, 1, M, K, kk, static_cast<const float *>(D), ldd, nullptr, w, ldw, nullptr, 0, f32_out(dX), dX->ld, nullptr, 0, nullptr, &ws, st);
+    auto run = [&]() -> int {
+        int r = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, zp, d0, dp, db, &ws, st);
+        if (!r && few) r = few_rows();
+        if (r || !split) return r;
+        const ff_row_parts xr = {scan(X), nullptr, 0, 0, ex_x, nullptr, nullptr};
+        const ff_row_parts dr = {{static_cast<const float *>(D), M, ldd, ldd}, const_cast<u16 *>(d[0].p), d[0].ld, d[0].plane, ex_d, ex_x, any_dw ? words.key : nullptr};
+        if (any_dw) r = sgnn_launch_ff_row_parts(ctx, xr, 0, nullptr, nullptr, st);
+        if (!r) r = sgnn_launch_ff_row_parts(ctx, dr, nw, wscan, words.largest, st);
+        if (!r) r = sgnn_launch_ff_parts(ctx, jobs, job, st);
+        if (!r && any_dw) r = weights(2, x, d, nullptr, words.ex + 1);
+        if (!r && tiles_dx) r = sgnn_launch_ff_nt(ctx, 2, M, K, N, n, d, w, ex_d, words.ex, view(dX), &ws, st);
+        return r;
+    };
+    return split ? sgnn_ff_close(ctx, run(), st) : run();
 }
 
 } // namespace
@@ -254,9 +272,8 @@ int sgnn_ctx_reserve_ffn(sgnn_ctx *ctx, uint64_t rows, uint32_t d_in, uint32_t d
     int rc = bind(ctx);
     if (rc) return rc;
     const uint64_t di = ff_pad8(d_in), dn = ff_pad8(d_out);
-    // fp32 split products: at most 256 ranges of the reduction, and 2304 tiles of 256 x 128 over all ranges
-    const uint64_t split = std::min<uint64_t>(2304ull * 256 * 128 * 4, d_in >= 4096 || d_out >= 4096 ? ~0ull : 257 * 4 * di * dn) + 257 * 4 * std::max(di, dn);
-    size_t need = rows * (2 * dn * 4 + di * 2) + 2 * di * dn * 4 * 2 + split + sgnn_ff_tn_ws_bytes(rows, di, dn) + sgnn_ff_sums_ws_bytes(dn) + sgnn_ff_rows_ws_bytes() + 16 * 256;
+    // fp32: both gradients of the pre-activations and their parts, the parts of X and of both weights; bfloat16 needs less
+    size_t need = rows * (2 * dn * 8 + di * 4 + 8) + 2 * di * dn * 4 + std::max(sgnn_ff_gemm_ws_bytes(di, dn), sgnn_ff_rows_ws_bytes()) + sgnn_ff_sums_ws_bytes(dn) + 16 * 256;
     need = std::max(need, sgnn_block_norm_ws_bytes(std::max(d_in, d_out)));
     if (need > ctx->ws_bytes) {
         SGNN_HIP(ctx, hipDeviceSynchronize());

@@ -1,7 +1,8 @@
 // The element-wise kernels of the feed-forward operators: bound by the bytes they move.
 //   act_bwd  D = dY * act'(Z), gated D0 = dY * U * act'(G), D1 = dY * act(G), and the column sums of either (the gradients of the biases), taken
 //            in fp32 before the rounding.  One read of each operand, one write of each result.
-//   apply    Y = act(Z) + R, gated Y = act(G) * U, fp32
+//   row_parts, parts   an fp32 matrix as two planes of fp16 parts, scaled by powers of two (ff_gemm.hip says how and why): by one for each row from the
+//            row's largest magnitude, or by a given one
 //   pack     a matrix as the tile kernel takes it: bfloat16, rows padded with zeros to whole 16-byte chunks
 // A workgroup has a strip of 32 chunks of columns (16 bytes a lane, 512 a row) and eight rows at a time.  Column sums: a thread adds up its rows, the
 // eight rows of threads meet in LDS, every workgroup writes one partial sum a column, and a second kernel adds these in a fixed order.
@@ -19,6 +20,27 @@ struct ffe_args {
     ff_mat dY, Z0, Z1, D0, D1;
     float *partial;                   // [gridDim.y][1 or 2][cols] or null
 };
+
+// Magnitudes are compared as the bits they have, which are in the same order (and tell the smallest ones from zero in every mode of the arithmetic).
+__device__ __forceinline__ uint32_t finite_max(uint32_t m, float v)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+    return b < 0x7f800000u ? max(m, b) : m;
+}
+
+// The workgroup's largest m into *word.  A workgroup that has nothing larger than what it reads leaves the word alone (2048 atomic operations on one
+// word would be the longest part of a small matrix).
+__device__ __forceinline__ void block_max(uint32_t m, uint32_t *word)
+{
+    __shared__ uint32_t red[4];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    const uint32_t t = max(max(red[0], red[1]), max(red[2], red[3]));
+    if (t > __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) __hip_atomic_fetch_max(word, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 template <int T, int V, bool GATED> __global__ __launch_bounds__(256) void ff_act_bwd_kernel(ffe_args a)
 {
@@ -90,27 +112,6 @@ __global__ __launch_bounds__(1024) void ff_colsum_kernel(const float *__restrict
     }
 }
 
-template <bool GATED> __global__ __launch_bounds__(256) void ff_apply_kernel(ffe_args a)
-{
-    constexpr int V = 4;
-    const int col = (blockIdx.x * FFE_CH + threadIdx.x % FFE_CH) * V, left = a.cols - col;
-    if (left <= 0) return;
-    for (int64_t row = (int64_t)blockIdx.y * FFE_ROWS + threadIdx.x / FFE_CH; row < a.rows; row += (int64_t)gridDim.y * FFE_ROWS) {
-        float g[V], u[V], y[V];
-        ff_load<FF_T32, V>(g, a.Z0, row, col, left);
-        if (a.Z1.p) ff_load<FF_T32, V>(u, a.Z1, row, col, left);
-        ff_with_act(a.act, [&](auto act) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                y[i] = ff_act<decltype(act)::value>(g[i]);
-                if (GATED) y[i] *= u[i];
-                else if (a.Z1.p) y[i] += u[i];
-            }
-        });
-        ff_store<FF_T32, V>(y, a.D0, row, col, left);
-    }
-}
-
 template <int T> __global__ __launch_bounds__(256) void ff_pack_kernel(ff_mat src, int64_t rows, int cols, int pcols, ff_mat dst)
 {
     const int chunks = pcols / 8;
@@ -124,17 +125,101 @@ template <int T> __global__ __launch_bounds__(256) void ff_pack_kernel(ff_mat sr
     }
 }
 
-__global__ __launch_bounds__(256) void ff_copy32_kernel(ff_mat src, int64_t rows, int cols, int pcols, ff_mat dst)
+// f(row, first column) for the chunks of V columns of a matrix, dealt to the threads of gridDim.x workgroups
+template <int V, class F> __device__ __forceinline__ void for_chunks(int64_t rows, int64_t cols, F f)
 {
-    const int chunks = (pcols + 3) / 4;
-    const int64_t n = rows * chunks;
+    const int64_t chunks = (cols + V - 1) / V, n = rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / chunks;
-        const int col = 4 * (int)(i % chunks);
-        float v[4];
-        ff_load<FF_T32, 4>(v, src, row, col, cols - col);
-        ff_store<FF_T32, 4>(v, dst, row, col, pcols - col);
+        const int64_t row = n <= 0xffffffffll ? (int64_t)((uint32_t)i / (uint32_t)chunks) : i / chunks;
+        f(row, V * (i - row * chunks));
     }
+}
+
+__device__ __forceinline__ int exponent_of(uint32_t bits, int none) { return bits ? 14 + 127 - (int)(bits >> 23) : none; }
+
+// eight values times 2^ex as their parts
+__device__ __forceinline__ void store_parts(const float (&v)[8], int ex, u16 *to, int64_t plane)
+{
+    _Float16 h[2][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_amdgcn_ldexpf(v[e], ex);
+        h[0][e] = (_Float16)x;
+        const float r = (x - (float)h[0][e]) * 2048.f;
+        h[1][e] = (_Float16)(fabsf(x) < __builtin_inff() ? r : 0.f);
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) *reinterpret_cast<u32x4 *>(to + q * plane) = *reinterpret_cast<const u32x4 *>(h[q]);
+}
+
+struct ffe_rows { ff_row_parts r; ff_scan w[2]; uint32_t *word; };
+
+// G lanes a row; CH chunks of eight values a lane stay in registers, or (CH = 0) a row is read once for its largest magnitude and once for its parts
+template <int G, int CH> __global__ __launch_bounds__(256) void ff_row_parts_kernel(ffe_rows s)
+{
+    if (blockIdx.y > 0) {
+        const ff_scan &m = s.w[blockIdx.y - 1];
+        const ff_mat src = {m.p, m.ld, 0};
+        uint32_t largest = 0;
+        for_chunks<8>(m.rows, m.cols, [&](int64_t row, int64_t col) {
+            float v[8];
+            ff_load<FF_T32, 8>(v, src, row, col, (int)min(m.cols - col, (int64_t)8));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) largest = finite_max(largest, v[e]);
+        });
+        block_max(largest, s.word);
+        return;
+    }
+    const ff_row_parts &p = s.r;
+    const ff_mat src = {p.m.p, p.m.ld, 0};
+    const int l = threadIdx.x % G;
+    const int64_t chunks = (p.m.cols + 7) / 8;
+    int key = 0;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < p.m.rows; row += (int64_t)gridDim.x * (256 / G)) {
+        float v[CH ? CH : 1][8];
+        uint32_t largest = 0;
+        auto each = [&](auto f) {
+            if constexpr (CH > 0) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    if (c * G + l < chunks) f(v[c], (int64_t)8 * (c * G + l));
+            } else
+                for (int64_t c = l; c < chunks; c += G) f(v[0], 8 * c);
+        };
+        auto load = [&](float (&x)[8], int64_t col) { ff_load<FF_T32, 8>(x, src, row, col, (int)min(p.m.cols - col, (int64_t)8)); };
+        if constexpr (CH > 0) each(load);          // all of them requested together
+        each([&](float (&x)[8], int64_t col) {
+            if constexpr (CH == 0) load(x, col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) largest = finite_max(largest, x[e]);
+        });
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, o, 64));
+        const int ex = exponent_of(largest, FF_EX_ZERO);
+        if (l == 0) p.ex[row] = ex;
+        if (p.other) key = max(key, FF_EX_KEY - ex - p.other[row]);
+        if (p.to)
+            each([&](float (&x)[8], int64_t col) {
+                if constexpr (CH == 0) load(x, col);
+                store_parts(x, ex, p.to + row * p.ld + col, p.plane);
+            });
+    }
+    if (p.key) block_max((uint32_t)key, p.key);
+}
+
+struct ffe_parts { ff_parts m[3]; };
+
+__global__ __launch_bounds__(256) void ff_parts_kernel(ffe_parts s)
+{
+    const ff_parts &p = s.m[blockIdx.y];
+    const ff_mat src = {p.m.p, p.m.ld, 0};
+    const int ex = p.rows ? FF_EX_KEY - (int)*p.word : exponent_of(*p.word, 0);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.ex = ex;
+    for_chunks<8>(p.m.rows, p.m.cols, [&](int64_t row, int64_t col) {
+        float v[8];
+        ff_load<FF_T32, 8>(v, src, row, col, (int)min(p.m.cols - col, (int64_t)8));
+        store_parts(v, p.rows ? ex - p.rows[row] : ex, p.to + row * p.ld + col, p.plane);
+    });
 }
 
 __global__ __launch_bounds__(256) void ff_zero_kernel(ff_mat m, int64_t rows, int64_t cols)
@@ -192,18 +277,6 @@ int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pc
     return SGNN_OK;
 }
 
-int sgnn_launch_ff_apply(sgnn_ctx *ctx, int64_t rows, int64_t cols, int act, const ff_mat &Z0, const ff_mat *Z1, const ff_mat &R, const ff_mat &Y, hipStream_t st)
-{
-    ffe_args a = {};
-    a.rows = rows; a.cols = (int)cols; a.act = act;
-    a.Z0 = Z0; a.Z1 = Z1 ? *Z1 : R; a.D0 = Y;
-    const unsigned strips = cdiv(cols, FFE_CH * 4);
-    const dim3 grid(strips, row_blocks(rows, strips));
-    if (Z1) SGNN_LAUNCH(ctx, st, "ff_apply_kernel", SGNN_TAG, ff_apply_kernel<true>, grid, dim3(256), 0, st, a);
-    else SGNN_LAUNCH(ctx, st, "ff_apply_kernel", SGNN_TAG, ff_apply_kernel<false>, grid, dim3(256), 0, st, a);
-    return SGNN_OK;
-}
-
 int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, u16 *dst, int64_t ldd, hipStream_t st)
 {
     const int64_t pcols = ff_pad8(cols);
@@ -214,10 +287,42 @@ int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t 
     return SGNN_OK;
 }
 
-int sgnn_launch_ff_copy32(sgnn_ctx *ctx, const float *src, int64_t lds_, int64_t rows, int64_t cols, int64_t pcols, float *dst, int64_t ldd, hipStream_t st)
+int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *word, hipStream_t st)
 {
-    const ff_mat s = {src, lds_, 0}, d = {dst, ldd, 0};
-    SGNN_LAUNCH(ctx, st, "ff_copy32_kernel", SGNN_TAG, ff_copy32_kernel, dim3(flat_blocks(rows * ((pcols + 3) / 4))), dim3(256), 0, st, s, rows, (int)cols, (int)pcols, d);
+    ffe_rows s = {};
+    s.r = r;
+    s.word = word;
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        s.w[i] = w[i];
+        most = std::max(most, w[i].rows * w[i].cols);
+    }
+    const int64_t chunks = cdiv(r.m.cols, 8);
+    auto run = [&](auto g, auto ch) -> int {
+        constexpr int G = decltype(g)::value, CH = decltype(ch)::value;
+        const unsigned blocks = (unsigned)std::min<int64_t>(std::max<int64_t>(cdiv(r.m.rows, 256 / G), std::min<int64_t>(cdiv(most, 256 * 8), 512)), 4096);
+        SGNN_LAUNCH(ctx, st, "ff_row_parts_kernel", SGNN_TAG, (ff_row_parts_kernel<G, CH>), dim3(blocks, 1 + n), dim3(256), 0, st, s);
+        return SGNN_OK;
+    };
+    // the fewest lanes that hold a row, one chunk each up to a wavefront
+    if (chunks <= 16) return run(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    if (chunks <= 32) return run(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
+    if (chunks <= 64) return run(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    if (chunks <= 128) return run(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    if (chunks <= 256) return run(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+    return run(std::integral_constant<int, 64>(), std::integral_constant<int, 0>());
+}
+
+int sgnn_launch_ff_parts(sgnn_ctx *ctx, int n, const ff_parts *m, hipStream_t st)
+{
+    ffe_parts s = {};
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        s.m[i] = m[i];
+        most = std::max(most, m[i].m.rows * (m[i].m.cols + 7));
+    }
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(cdiv(most, 256 * 8), 4096));
+    SGNN_LAUNCH(ctx, st, "ff_parts_kernel", SGNN_TAG, ff_parts_kernel, dim3(blocks, n), dim3(256), 0, st, s);
     return SGNN_OK;
 }
 

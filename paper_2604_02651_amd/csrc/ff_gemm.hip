@@ -13,6 +13,16 @@
 // and columns behind the edge of the matrix repeat the last ones and feed results that are never stored.
 // v_mfma_f32_32x32x16_bf16 computes the transposed tile: register r of lane (kh, li) is row li, column 8 (r / 4) + 4 kh + r % 4 of a
 // block: four adjacent columns a lane, which the epilogue brings to eight through LDS.
+//
+// fp32 products take the same path on the fp16 pipe.  Values are scaled by powers of two, the largest magnitude of a row (of X, of the gradients) or of
+// a weight matrix to [2^14, 2^15), and every one is split into two fp16 parts (ff_elem.hip):
+//   x = x1 + 2^-11 x2,  x1 = fp16(x), x2 = fp16(2^11 (x - x1)),  |error| <= 2^-23 |x|
+//   a b = a1 b1 + 2^-11 (a1 b2 + a2 b1) + up to 2^-21 |a b| (the product of the second parts, and what the parts leave out)
+// three products of exact terms, the leading ones and the others in accumulators of their own.  The method is that of Ootomo and Yokota, "Recovering
+// single precision accuracy from Tensor Cores while surpassing the FP32 theoretical peak performance" (2022).  The second part's own scale keeps all of
+// its bits down to 2^-29 of the largest value; smaller values are off by up to 2^-51 of it.  For tn, where the reduction is along the rows, row m of X is
+// scaled so that all of x d have one scale: the largest products keep their bits, rows that add nothing count for nothing.  An infinity or NaN is its
+// own first part with a second part of 0, and a sum of first parts that is not finite is the result.
 #include "ff.h"
 #include "ff_act.h"
 
@@ -21,18 +31,22 @@ namespace {
 // what a load behind the end of the reduction brings
 __device__ const u32x4 ff_zeros = {0u, 0u, 0u, 0u};
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 enum { FFK_LINEAR = 0, FFK_GLU = 1, FFK_PARTIAL = 2 };
 
 struct ffg_args {
     int64_t M, K;
     int N;                            // columns of one result matrix
     int segs, mats;                   // nt: segments of the reduction; tn: results side by side
-    const u16 *A[2]; int64_t lda;
-    const u16 *B[2]; int64_t ldb[2];  // of each segment, result or projection; ldb[1] of the second projection only
+    ff_op A[2], B[2];                 // A of each segment, B of each segment, result or projection (of the first two one leading dimension)
+    const int32_t *ex_rows, *ex;      // fp32: the exponents by which the rows of A (or null) and everything else were scaled
     ff_epilogue e;
     uint32_t mtiles, ntiles, splits;  // ntiles of one matrix
     int slices, per_split;            // slices of BK along the whole reduction, and of one range of it
-    float *partial;                   // [splits][mats][M][N]
+    float *partial;                   // tn: [splits][mats][M][N]; else, where the reduction is split: [tiles][splits][BM BN]
+    uint32_t *arrived;                // [tiles], zero between calls
+    uint32_t *clear;                  // two words that the next call wants at zero, or null
 };
 
 // Operand of R rows (or columns) by BK reduction steps in LDS
@@ -46,17 +60,20 @@ template <int R, int BK, bool TR> struct ffg_operand {
     }
 };
 
-template <int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR, int KIND>
-__global__ __launch_bounds__(64 * WM * WN, BM * BN >= 65536 ? 2 : 1) void ff_gemm_kernel(ffg_args a)
+// PL: 1 bfloat16, 2 fp32 as two planes of fp16 parts
+template <int PL, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR, int KIND>
+__global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void ff_gemm_kernel(ffg_args a)
 {
     // gated: the tile's columns are half of B0's, half of B1's, each an operand of its own in LDS
     constexpr int PARTS = KIND == FFK_GLU ? 2 : 1, BNP = BN / PARTS;
     using OA = ffg_operand<BM, BK, ATR>;
     using OB = ffg_operand<BNP, BK, BTR>;
-    constexpr int NW = WM * WN, TM = BM / 32 / WM, TN = BN / 32 / WN, STAGE = OA::BYTES + PARTS * OB::BYTES;
-    constexpr int AJ = OA::BYTES / 1024 / NW, BJ = OB::BYTES / 1024 / NW, LOADS = AJ + PARTS * BJ;
-    static_assert(OA::BYTES % (1024 * NW) == 0 && OB::BYTES % (1024 * NW) == 0, "a wavefront's loads are of one operand each");
-    static_assert(KIND != FFK_GLU || (TN == 2 && BTR), "a wavefront has the same columns of both projections");
+    // a slice in LDS: the planes of A, then for each part the planes of B; loads of 1 KB (a wavefront's), load l of the slice by wavefront l % NW
+    constexpr int NW = WM * WN, TM = BM / 32 / WM, TN = BN / 32 / WN, STAGE = PL * (OA::BYTES + PARTS * OB::BYTES);
+    constexpr int AL = OA::BYTES / 1024, BL = OB::BYTES / 1024, LOADS = STAGE / 1024 / NW;
+    constexpr bool EVEN = AL % NW == 0 && BL % NW == 0;         // which operand a load is of does not depend on the wavefront
+    static_assert(OA::BYTES % 1024 == 0 && OB::BYTES % 1024 == 0 && STAGE % (1024 * NW) == 0, "whole loads, as many for every wavefront");
+    static_assert(KIND != FFK_GLU || (TN % 2 == 0 && BTR), "a wavefront has the same columns of both projections");
     extern __shared__ __attribute__((aligned(16))) unsigned char ffg_smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 31, kh = lane >> 5;
     const int wm = wave / WN, wn = wave % WN;
@@ -66,6 +83,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN >= 65536 ? 2 : 1) void ff_gem
     const uint32_t per_mat = a.mtiles * a.ntiles, tiles = per_mat * a.mats * a.splits, run = (tiles + 7) / 8;
     const uint32_t id = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= run || id >= tiles) return;
+    if (a.clear && id == 0 && threadIdx.x < 2) a.clear[threadIdx.x] = 0;
     const uint32_t z = id / (per_mat * a.mats), t = id % (per_mat * a.mats), cols = a.ntiles * a.mats, group = t / (4 * cols);
     const uint32_t gm = min(4u, a.mtiles - 4 * group), in = t % (4 * cols);
     const uint32_t bm = 4 * group + in % gm, bc = in / gm, mat = bc / a.ntiles, bn = bc % a.ntiles;
@@ -73,53 +91,55 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN >= 65536 ? 2 : 1) void ff_gem
     const int n0 = (int)bn * BNP;
     const int s0 = (int)z * a.per_split, nslices = min(a.slices - s0, a.per_split), seg_slices = (int)((a.K + BK - 1) / BK);
 
-    // A lane's place in the wave-loads of a slice: load j of an operand fills KB wave + NW j of its part.  off: bytes from the tile's first value.
-    uint32_t off_a[AJ], off_b[PARTS][BJ];
-    auto place = [&](auto op, int j, int &line, int &chunk) {
-        using O = decltype(op);
-        const int p = (wave + NW * j) * 64 + lane;
-        line = p / O::CH;
-        chunk = (p % O::CH) ^ O::swizzle(line);
+    // load j of the wavefront: of which part of the slice, and the lane's place in it
+    struct place { bool b; int sub, line, chunk; };
+    auto where = [&](int j) {
+        const int l = (EVEN ? 0 : wave) + NW * j;
+        place p;
+        p.b = l >= PL * AL;
+        p.sub = p.b ? (l - PL * AL) / BL : l / AL;
+        const int at = ((p.b ? (l - PL * AL) % BL : l % AL) + (EVEN ? wave : 0)) * 64 + lane;
+        p.line = p.b ? at / OB::CH : at / OA::CH;
+        p.chunk = p.b ? (at % OB::CH) ^ OB::swizzle(p.line) : (at % OA::CH) ^ OA::swizzle(p.line);
+        return p;
     };
-    auto offset = [&](auto op, bool tr, int j, int64_t ld, int64_t lines_left) {
-        int line, c;
-        place(op, j, line, c);
-        const int64_t last = lines_left - 1;
-        return tr ? (uint32_t)line * (uint32_t)(2 * ld) + 16u * (uint32_t)min((int64_t)c, last / 8) : (uint32_t)min((int64_t)line, last) * (uint32_t)(2 * ld) + 16u * (uint32_t)c;
-    };
+    uint32_t off[LOADS];          // bytes from the tile's first value
 #pragma unroll
-    for (int j = 0; j < AJ; ++j) off_a[j] = offset(OA(), ATR, j, a.lda, a.M - m0);
-#pragma unroll
-    for (int q = 0; q < PARTS; ++q)
-#pragma unroll
-        for (int j = 0; j < BJ; ++j) off_b[q][j] = offset(OB(), BTR, j, a.ldb[q], a.N - n0);
+    for (int j = 0; j < LOADS; ++j) {
+        const place p = where(j);
+        const bool tr = p.b ? BTR : ATR;
+        const int64_t last = p.b ? a.N - 1 - n0 : a.M - 1 - m0, ld = p.b ? a.B[KIND == FFK_GLU ? p.sub / PL : 0].ld : a.A[0].ld;
+        off[j] = tr ? (uint32_t)p.line * (uint32_t)(2 * ld) + 16u * (uint32_t)min((int64_t)p.chunk, last / 8)
+                    : (uint32_t)min((int64_t)p.line, last) * (uint32_t)(2 * ld) + 16u * (uint32_t)p.chunk;
+    }
     auto issue = [&](int s) {
         const int sl = s0 + min(s, nslices - 1);        // past the end: the last slice again, into a stage nobody reads
         const int seg = a.segs > 1 && sl >= seg_slices ? 1 : 0;
         const int64_t k0 = (int64_t)(sl - seg * seg_slices) * BK;
         unsigned char *stage = ffg_smem + (s % STAGES) * STAGE + 1024 * wave;
         const int left = (int)min(a.K - k0, (int64_t)BK);
-        auto part = [&](auto op, bool tr, auto &off, const u16 *first, unsigned char *to) {
-            constexpr int J = sizeof(off) / sizeof(off[0]);
-            const unsigned char *g = reinterpret_cast<const unsigned char *>(first);
-            if (left >= BK) {
-#pragma unroll
-                for (int j = 0; j < J; ++j) __builtin_amdgcn_global_load_lds(STREAM_GPTR(g + off[j]), STREAM_LPTR(to + 1024 * NW * j), 16, 0, 0);
-            } else {
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    int line, c;
-                    place(op, j, line, c);
-                    const unsigned char *p = (tr ? line : 8 * c) < left ? g + off[j] : reinterpret_cast<const unsigned char *>(&ff_zeros);
-                    __builtin_amdgcn_global_load_lds(STREAM_GPTR(p), STREAM_LPTR(to + 1024 * NW * j), 16, 0, 0);
-                }
-            }
-        };
-        part(OA(), ATR, off_a, a.A[seg] + (ATR ? k0 * a.lda + m0 : m0 * a.lda + k0), stage);
+        const u16 *first_a = a.A[seg].p + (ATR ? k0 * a.A[0].ld + m0 : m0 * a.A[0].ld + k0);
+        const u16 *first_b[PARTS];
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
             const int which = KIND == FFK_GLU ? q : (KIND == FFK_PARTIAL ? (int)mat : seg);
-            part(OB(), BTR, off_b[q], a.B[which] + (BTR ? k0 * a.ldb[q] + n0 : (int64_t)n0 * a.ldb[q] + k0), stage + OA::BYTES + q * OB::BYTES);
+            const int64_t ld = a.B[KIND == FFK_GLU ? q : 0].ld;
+            first_b[q] = a.B[which].p + (BTR ? k0 * ld + n0 : (int64_t)n0 * ld + k0);
+        }
+        auto base = [&](const place &p) {
+            const int plane = PL > 1 ? p.sub % PL : 0, q = PARTS > 1 ? p.sub / PL : 0;
+            return reinterpret_cast<const unsigned char *>(p.b ? first_b[q] + plane * a.B[KIND == FFK_GLU ? q : 0].plane : first_a + plane * a.A[0].plane);
+        };
+        if (left >= BK) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) __builtin_amdgcn_global_load_lds(STREAM_GPTR(base(where(j)) + off[j]), STREAM_LPTR(stage + 1024 * NW * j), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const place p = where(j);
+                const unsigned char *g = ((p.b ? BTR : ATR) ? p.line : 8 * p.chunk) < left ? base(p) + off[j] : reinterpret_cast<const unsigned char *>(&ff_zeros);
+                __builtin_amdgcn_global_load_lds(STREAM_GPTR(g), STREAM_LPTR(stage + 1024 * NW * j), 16, 0, 0);
+            }
         }
     };
 
@@ -138,17 +158,20 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN >= 65536 ? 2 : 1) void ff_gem
     for (int i = 0; i < TM; ++i) at_a[i] = ATR ? tr_at(OA(), wm * TM + i) : kc_at(OA(), wm * TM + i);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-        const int blk = KIND == FFK_GLU ? wn : wn * TN + j;
-        at_b[j] = OA::BYTES + (KIND == FFK_GLU ? j * OB::BYTES : 0) + (BTR ? tr_at(OB(), blk) : kc_at(OB(), blk));
+        const int blk = KIND == FFK_GLU ? wn * (TN / 2) + j % (TN / 2) : wn * TN + j;
+        at_b[j] = PL * OA::BYTES + (KIND == FFK_GLU ? j / (TN / 2) * PL * OB::BYTES : 0) + (BTR ? tr_at(OB(), blk) : kc_at(OB(), blk));
     }
 
-    f32x16 acc[TM][TN];
+    f32x16 acc[TM][TN], low[PL > 1 ? TM : 1][PL > 1 ? TN : 1];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+            for (int r = 0; r < 16; ++r) {
+                acc[i][j][r] = 0.f;
+                if (PL > 1) low[PL > 1 ? i : 0][PL > 1 ? j : 0][r] = 0.f;
+            }
 
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(s);
@@ -161,26 +184,89 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN >= 65536 ? 2 : 1) void ff_gem
         const unsigned char *stage = ffg_smem + (s % STAGES) * STAGE;
 #pragma unroll
         for (int ks = 0; ks < BK / 16; ++ks) {
-            bf16x8 fa[TM], fb[TN];
+            u32x4 fa[PL][TM], fb[PL][TN];
             auto fetch = [&](auto op, bool tr, int at) {
                 using O = decltype(op);
                 if (tr) {
                     const uint2 lo = read_tr(stage + at + 16 * ks * O::ROW), hi = read_tr(stage + at + (16 * ks + 4) * O::ROW);
-                    return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+                    return u32x4{lo.x, lo.y, hi.x, hi.y};
                 }
                 return read_row(stage + (at ^ (32 * ks)));
             };
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = fetch(OB(), BTR, at_b[j]);
+            for (int p = 0; p < PL; ++p) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = fetch(OA(), ATR, at_a[i]);
+                for (int j = 0; j < TN; ++j) fb[p][j] = fetch(OB(), BTR, at_b[j] + p * OB::BYTES);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i) fa[p][i] = fetch(OA(), ATR, at_a[i] + p * OA::BYTES);
+            }
+            auto multiply = [&](auto &c, int pa, int pb) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        if constexpr (PL > 1) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fb[pb][j]), __builtin_bit_cast(f16x8, fa[pa][i]), c[i][j], 0, 0, 0);
+                        else c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[pb][j]), __builtin_bit_cast(bf16x8, fa[pa][i]), c[i][j], 0, 0, 0);
+                    }
+            };
+            multiply(acc, 0, 0);
+            if constexpr (PL > 1) {
+                multiply(low, 1, 0);
+                multiply(low, 0, 1);
+            }
         }
     }
     STREAM_WAIT_VMCNT(0);       // the repeated loads past the end are still in flight: nothing may leave before they land
+    if constexpr (PL > 1) {
+        const int ex = *a.ex;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int64_t row = m0 + 32 * (wm * TM + i) + li;
+            const int back = -(a.ex_rows && row < a.M ? ex + a.ex_rows[row] : ex);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float h = acc[i][j][r];
+                    acc[i][j][r] = __builtin_amdgcn_ldexpf(fabsf(h) < __builtin_inff() ? fmaf(low[i][j][r], 0x1p-11f, h) : h, back);
+                }
+        }
+    }
+    if constexpr (KIND != FFK_PARTIAL) {
+        if (a.splits > 1) {
+            // every range leaves its sums, past the XCD's own L2; the workgroup that arrives last adds them up in their order and goes on
+            __shared__ uint32_t last;
+            float *const to = a.partial + ((size_t)t * a.splits + z) * (BM * BN) + wave * (TM * TN * 1024) + lane;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) __hip_atomic_store(to + ((i * TN + j) * 16 + r) * 64, acc[i][j][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            STREAM_WAIT_VMCNT(0);
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                last = __hip_atomic_fetch_add(a.arrived + t, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (last == a.splits - 1) __hip_atomic_store(a.arrived + t, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            if (last != a.splits - 1) return;
+            const float *const from = a.partial + (size_t)t * a.splits * (BM * BN) + wave * (TM * TN * 1024) + lane;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    f32x16 sum;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+                    for (uint32_t y = 0; y < a.splits; ++y)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            sum[r] += __hip_atomic_load(from + (size_t)y * (BM * BN) + ((i * TN + j) * 16 + r) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    acc[i][j] = sum;
+                }
+        }
+    }
 
     // A wavefront's blocks go through a strip of LDS of its own, 32 rows at a time, so that a lane has eight adjacent columns and rows leave (and the
     // residual is read) in pieces of 64 bytes and more.
@@ -224,8 +310,8 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN >= 65536 ? 2 : 1) void ff_gem
             };
             read(v, 0);
             if constexpr (KIND == FFK_PARTIAL) {
-                const ff_mat o = {a.partial + ((int64_t)z * a.mats + mat) * a.M * a.N, a.N, 0};
-                ff_store<FF_T32, 8>(v, o, row, col, cols_left);
+                if (a.splits == 1) ff_store<FF_TANY, 8>(v, mat ? ep.Z[0] : ep.Y, row, col, cols_left);
+                else ff_store<FF_T32, 8>(v, ff_mat{a.partial + ((int64_t)z * a.mats + mat) * a.M * a.N, a.N, 0}, row, col, cols_left);
             } else {
                 if (KIND == FFK_GLU) read(u, EC);
 #pragma unroll
@@ -268,79 +354,147 @@ __global__ __launch_bounds__(256) void ff_reduce_kernel(const float *__restrict_
     ff_store<FF_TANY, 4>(s, mat ? C1 : C0, row, col, left);
 }
 
-template <int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR, int KIND> int launch(sgnn_ctx *ctx, ffg_args a, int64_t per_split, hipStream_t st)
+template <int PL, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR, int KIND> int launch(sgnn_ctx *ctx, ffg_args a, int64_t splits, ws_alloc *ws, hipStream_t st)
 {
-    constexpr int LDS = STAGES * (BM + BN) * BK * 2;
+    constexpr int LDS = STAGES * PL * (BM + BN) * BK * 2;
     a.mtiles = cdiv(a.M, BM);
     a.ntiles = cdiv(a.N, KIND == FFK_GLU ? BN / 2 : BN);
     const int64_t slices = (int64_t)a.segs * cdiv(a.K, BK);
     a.slices = (int)slices;
-    a.per_split = KIND == FFK_PARTIAL ? (int)per_split : (int)slices;
+    a.per_split = (int)cdiv(slices, splits);
     a.splits = cdiv(slices, a.per_split);
     const uint64_t tiles = (uint64_t)a.mtiles * a.ntiles * a.mats * a.splits;
     if (tiles > 0x70000000ull || slices > 0x7fffffff) return sgnn_fail(ctx, SGNN_ERR_UNSUPPORTED, "feed-forward product: more than 2^31 tiles");
-    SGNN_HIP(ctx, (sgnn_allow_lds<&ff_gemm_kernel<BM, BN, WM, WN, BK, STAGES, ATR, BTR, KIND>>(ctx, LDS)));
+    const bool joined = KIND != FFK_PARTIAL && a.splits > 1;
+    if (a.splits > 1) {
+        a.partial = ws->get<float>(KIND == FFK_PARTIAL ? (size_t)a.splits * a.mats * a.M * a.N : tiles * BM * BN);
+        if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
+    }
+    if (joined) {
+        a.arrived = sgnn_ff_words(ctx).arrived;
+        const int rc = sgnn_ff_open(ctx, st);
+        if (rc) return rc;
+    }
+    SGNN_HIP(ctx, (sgnn_allow_lds<&ff_gemm_kernel<PL, BM, BN, WM, WN, BK, STAGES, ATR, BTR, KIND>>(ctx, LDS)));
     char tag[56] = "";
-    if (ctx->prof_on) snprintf(tag, sizeof(tag), "%c%c%s %dx%d %lldx%dx%lld", ATR ? 'T' : 'N', BTR ? 'N' : 'T', KIND == FFK_GLU ? " gated" : "", BM, BN, (long long)a.M, a.N, (long long)a.K);
-    SGNN_LAUNCH(ctx, st, "ff_gemm_kernel", tag, (ff_gemm_kernel<BM, BN, WM, WN, BK, STAGES, ATR, BTR, KIND>), dim3((unsigned)((tiles + 7) / 8 * 8)),
-                dim3(64 * WM * WN), LDS, st, a);
-    return SGNN_OK;
+    if (ctx->prof_on)
+        snprintf(tag, sizeof(tag), "%c%c%s %dx%d %lldx%dx%lld%s /%u", ATR ? 'T' : 'N', BTR ? 'N' : 'T', KIND == FFK_GLU ? " gated" : "", BM, BN, (long long)a.M, a.N,
+                 (long long)a.K, PL > 1 ? " f32" : "", a.splits);
+    auto go = [&]() -> int {
+        SGNN_LAUNCH(ctx, st, "ff_gemm_kernel", tag, (ff_gemm_kernel<PL, BM, BN, WM, WN, BK, STAGES, ATR, BTR, KIND>), dim3((unsigned)((tiles + 7) / 8 * 8)),
+                    dim3(64 * WM * WN), LDS, st, a);
+        return SGNN_OK;
+    };
+    int rc = go();
+    if (joined) rc = sgnn_ff_close(ctx, rc, st);
+    return rc;
+}
+
+// tile sizes, and ranges of the reduction
+enum { FFT_WIDE, FFT_TALL, FFT_MID, FFT_SMALL };
+
+// Tiles of BM x BN for a result of M x N (both projections counted), K steps of the reduction.
+int tile_for(int pl, int64_t M, int64_t N, int64_t K, int64_t *splits)
+{
+    auto tiles = [&](int64_t bm, int64_t bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn); };
+    *splits = 1;
+    if (pl == 1 ? tiles(256, 256) >= 192 : tiles(256, 128) >= 192) return pl == 1 && K <= 256 ? FFT_TALL : FFT_WIDE;
+    if (tiles(128, 128) >= 256) return FFT_MID;
+    const int64_t n = tiles(64, 128), slices = cdiv(K, pl == 1 ? 64 : 32);
+    if (n <= 256) *splits = std::max<int64_t>(1, std::min<int64_t>(512 / n, slices / 4));
+    return FFT_SMALL;
+}
+
+template <bool ATR, bool BTR, int KIND> int launch_tile(sgnn_ctx *ctx, int pl, const ffg_args &a, int tile, int64_t splits, ws_alloc *ws, hipStream_t st)
+{
+    if (pl == 1) {
+        if (tile == FFT_WIDE) return launch<1, 256, 256, 2, 4, 64, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+        if (tile == FFT_TALL) return launch<1, 256, 128, 2, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+        if (tile == FFT_MID) return launch<1, 128, 128, 2, 2, 64, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+        return launch<1, 64, 128, 2, 2, 64, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+    }
+    if (tile == FFT_WIDE || tile == FFT_TALL) return launch<2, 256, 128, 4, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+    if (tile == FFT_MID) return launch<2, 128, 128, 2, 2, 32, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+    return launch<2, 64, 128, 2, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+}
+
+// An fp32 product also clears the largest magnitudes: the parts have been made of them, and nothing reads them before the next call.
+ffg_args args(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const int32_t *ex_rows, const int32_t *ex)
+{
+    ffg_args a = {};
+    if (ex) a.clear = sgnn_ff_words(ctx).key;
+    a.M = M; a.N = (int)N; a.K = K; a.segs = a.mats = 1;
+    a.ex_rows = ex_rows; a.ex = ex;
+    a.e.act = SGNN_ACT_NONE;
+    return a;
 }
 
 } // namespace
 
-int sgnn_launch_ff_linear(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const u16 *A, int64_t lda, const u16 *B, int64_t ldb, const ff_epilogue &e,
-                          hipStream_t st)
+int sgnn_launch_ff_nn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
+                      const ff_epilogue &e, ws_alloc *ws, hipStream_t st)
 {
-    ffg_args a = {};
-    a.M = M; a.N = (int)N; a.K = K; a.segs = a.mats = 1;
-    a.A[0] = A; a.lda = lda; a.B[0] = B; a.ldb[0] = ldb; a.e = e;
-    return launch<128, 128, 2, 2, 64, 2, false, true, FFK_LINEAR>(ctx, a, 0, st);
-}
-
-int sgnn_launch_ff_glu(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const u16 *A, int64_t lda, const u16 *B0, int64_t ldb0, const u16 *B1, int64_t ldb1,
-                       const ff_epilogue &e, hipStream_t st)
-{
-    ffg_args a = {};
-    a.M = M; a.N = (int)N; a.K = K; a.segs = a.mats = 1;
-    a.A[0] = A; a.lda = lda; a.B[0] = B0; a.ldb[0] = ldb0; a.B[1] = B1; a.ldb[1] = ldb1; a.e = e;
-    return launch<128, 128, 2, 2, 64, 2, false, true, FFK_GLU>(ctx, a, 0, st);
-}
-
-int sgnn_launch_ff_nt(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int segs, const u16 *const *A, int64_t lda, const u16 *const *B, int64_t ldb,
-                      const ff_mat &Y, hipStream_t st)
-{
-    ffg_args a = {};
-    a.M = M; a.N = (int)N; a.K = K; a.segs = segs; a.mats = 1;
-    a.lda = lda;
-    for (int s = 0; s < segs; ++s) { a.A[s] = A[s]; a.B[s] = B[s]; a.ldb[s] = ldb; }
-    a.e.act = SGNN_ACT_NONE;
-    a.e.Y = Y;
-    return launch<128, 128, 2, 2, 64, 2, false, false, FFK_LINEAR>(ctx, a, 0, st);
-}
-
-size_t sgnn_ff_tn_ws_bytes(uint64_t rows, uint64_t d_in, uint64_t d_out)
-{
-    return 2 * 32 * d_in * d_out * 4 + 256;
-}
-
-int sgnn_launch_ff_tn(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int mats, const u16 *A, int64_t lda, const u16 *const *B, int64_t ldb, const ff_mat *C,
-                      ws_alloc *ws, hipStream_t st)
-{
-    ffg_args a = {};
-    a.M = M; a.N = (int)N; a.K = K; a.segs = 1; a.mats = mats;
-    a.A[0] = A; a.lda = lda;
-    for (int s = 0; s < mats; ++s) { a.B[s] = B[s]; a.ldb[s] = ldb; }
-    const int64_t slices = cdiv(K, 64), tiles = (int64_t)cdiv(M, 128) * cdiv(N, 128) * mats;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(32, slices / 4), 512 / tiles));
-    const int64_t per = cdiv(slices, splits);
+    ffg_args a = args(ctx, M, N, K, ex_rows, ex);
+    a.A[0] = a.A[1] = A;
+    a.B[0] = B[0];
+    a.B[1] = B[mats - 1];
+    a.e = e;
+    int64_t splits;
+    const int tile = tile_for(pl, M, mats * N, K, &splits);
     const size_t off = ws->off;
-    a.partial = ws->get<float>((size_t)cdiv(slices, per) * mats * M * N);
-    if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
-    const int rc = launch<128, 128, 2, 2, 64, 2, true, true, FFK_PARTIAL>(ctx, a, per, st);
-    if (rc) return rc;
-    SGNN_LAUNCH(ctx, st, "ff_reduce_kernel", SGNN_TAG, ff_reduce_kernel, dim3(cdiv(M * ((N + 3) / 4) * mats, 256)), dim3(256), 0, st, a.partial,
-                (int)cdiv(slices, per), mats, M, (int)N, C[0], C[mats - 1]);
+    const int rc = mats == 2 ? launch_tile<false, true, FFK_GLU>(ctx, pl, a, tile, splits, ws, st) : launch_tile<false, true, FFK_LINEAR>(ctx, pl, a, tile, splits, ws, st);
     ws->off = off;         // what the caller launches next on this stream may have the scratch
+    return rc;
+}
+
+int sgnn_launch_ff_nt(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int segs, const ff_op *A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
+                      const ff_mat &Y, ws_alloc *ws, hipStream_t st)
+{
+    ffg_args a = args(ctx, M, N, K, ex_rows, ex);
+    a.segs = segs;
+    for (int s = 0; s < segs; ++s) { a.A[s] = A[s]; a.B[s] = B[s]; }
+    a.e.Y = Y;
+    int64_t splits;
+    const int tile = tile_for(pl, M, N, segs * K, &splits);
+    const size_t off = ws->off;
+    const int rc = launch_tile<false, false, FFK_LINEAR>(ctx, pl, a, tile, splits, ws, st);
+    ws->off = off;
+    return rc;
+}
+
+// Scratch of the products: partial results of tn (at most 64 ranges of M x N, or 768 tiles of 256 x 256 over all of them), sums of split tiles (512 of 64 x 128 and those
+// that made them up to 256)
+size_t sgnn_ff_gemm_ws_bytes(uint64_t d_in, uint64_t d_out)
+{
+    return std::max<uint64_t>(std::min<uint64_t>(2 * 64 * d_in * d_out, std::max<uint64_t>(768ull * 65536, 2 * d_in * d_out)) * 4, 768ull * 64 * 128 * 4) + 512;
+}
+
+int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
+                      const ff_mat *C, ws_alloc *ws, hipStream_t st)
+{
+    ffg_args a = args(ctx, M, N, K, ex_rows, ex);
+    a.mats = mats;
+    a.A[0] = a.A[1] = A;
+    for (int s = 0; s < mats; ++s) a.B[s] = B[s];
+    a.e.Y = C[0];             // where the reduction is not split
+    a.e.Z[0] = C[mats - 1];
+    const int bk = pl == 1 ? 64 : 32;
+    const int64_t slices = cdiv(K, bk);
+    // the widest tile that leaves a range of eight slices and more to a workgroup a compute unit
+    auto tiles = [&](int64_t bm, int64_t bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn) * mats; };
+    auto ranges = [&](int64_t n, int64_t total) { return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, slices / 4), total / n)); };
+    int tile = FFT_SMALL;
+    int64_t n = tiles(64, 128), splits = ranges(n, 512);
+    const int64_t nw = pl == 1 ? tiles(256, 256) : tiles(256, 128), nm = tiles(128, 128);
+    if (M > 128 && N > 64 && nw * (slices / 8) >= 192) tile = FFT_WIDE, splits = ranges(nw, 256);
+    else if (M > 64 && nm * (slices / 4) >= 192) tile = FFT_MID, splits = ranges(nm, 512);
+    const size_t off = ws->off;
+    const int rc = launch_tile<true, true, FFK_PARTIAL>(ctx, pl, a, tile, splits, ws, st);
+    if (rc) return rc;
+    ws->off = off;         // the partial results stay where they are until the next launch
+    const int64_t per = cdiv(slices, splits);
+    if (per >= slices) return SGNN_OK;
+    SGNN_LAUNCH(ctx, st, "ff_reduce_kernel", SGNN_TAG, ff_reduce_kernel, dim3(cdiv(M * ((N + 3) / 4) * mats, 256)), dim3(256), 0, st,
+                reinterpret_cast<const float *>(ws->base + off), (int)cdiv(slices, per), mats, M, (int)N, C[0], C[mats - 1]);
     return SGNN_OK;
 }

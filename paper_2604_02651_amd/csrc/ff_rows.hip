@@ -205,7 +205,7 @@ template <int KIND, bool NN, int V, int RT, int MATS> __global__ __launch_bounds
 #pragma unroll
             for (int w = 0; w < NW; ++w) t += red[q][w][r][c];
             // past the XCD's own L2, so that no cache has to be written back before the count (with a fence for the whole device instead 24 x 4096 x 1024 took
-            // 47 us, FIXME here)
+            // 47 us, 9 here)
             __hip_atomic_store(to + (q * ROWS + r) * CB + c, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): this wavefront's sums are where every XCD sees them
@@ -266,9 +266,9 @@ template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, 
     const size_t off = ws->off;
     if (a.splits > 1) {
         a.partial = ws->get<float>((size_t)tiles * a.splits * MATS * ROWS * CB);
-        a.arrived = reinterpret_cast<uint32_t *>(ctx->persist + SGNN_PERSIST_FFN_OFF);
+        a.arrived = sgnn_ff_words(ctx).arrived;
         if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
-        const int rc = sgnn_zero_open(ctx, SGNN_ZERO_FFN, a.arrived, SGNN_PERSIST_FFN_BYTES, st);
+        const int rc = sgnn_ff_open(ctx, st);
         if (rc) return rc;
     }
     char tag[56] = "";
@@ -278,7 +278,7 @@ template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, 
         return SGNN_OK;
     };
     int rc = run();
-    if (a.splits > 1) rc = sgnn_zero_close(ctx, rc, SGNN_ZERO_FFN, a.arrived, SGNN_PERSIST_FFN_BYTES, st);
+    if (a.splits > 1) rc = sgnn_ff_close(ctx, rc, st);
     ws->off = off;         // what the caller launches next on this stream may have the scratch
     return rc;
 }
