@@ -127,6 +127,8 @@ size_t sgnn_ff_rows_ws_bytes();
 // ---- ff_elem.hip --------------------------------------------------------------------------------
 // dst [rows x ff_pad8(cols)] = src in bfloat16, zeros behind the last column
 int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, u16 *dst, int64_t ldd, hipStream_t st);
+// dst = src in dst's storage
+int sgnn_launch_ff_convert(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, const ff_mat &dst, hipStream_t st);
 // fp32 operands as two planes of fp16 parts [rows x ff_pad8(cols)], zeros behind the last column (ff_gemm.hip says how and why).
 struct ff_scan { const float *p; int64_t rows, cols, ld; };
 // The rows of one matrix, each scaled by a power of two of its own: 2^ex[row] takes the row's largest finite magnitude to [2^14, 2^15); FF_EX_ZERO
@@ -139,6 +141,7 @@ int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const 
 // each row.  *ex: the scale of the matrix, or FF_EX_KEY - *word
 struct ff_parts { ff_scan m; const uint32_t *word; const int32_t *rows; int32_t *ex; u16 *to; int64_t ld, plane; };
 int sgnn_launch_ff_parts(sgnn_ctx *ctx, int n, const ff_parts *m, hipStream_t st);
+// (D0 without memory: the column sums only)
 // D0 = dY * act'(Z0), or with Z1 D0 = dY * Z1 * act'(Z0) and D1 = dY * act(Z0); zeros in the columns from cols to pcols; column sums (before
 // the rounding) to db[0], db[1] where they are wanted
 int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pcols, int act, const ff_mat &dY, const ff_mat &Z0, const ff_mat *Z1,

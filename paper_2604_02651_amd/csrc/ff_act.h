@@ -23,10 +23,21 @@ __device__ __forceinline__ float ff_gelu_inner(float z)
     return 1.5957691216057308f * c * fmaf(0.044715f * c, c, 1.f);
 }
 
+// Phi(z) and the density phi(z), both from exp(-z^2 / 2): 1 - Phi = phi-like polynomial of 1 / (1 + p |z| / sqrt 2) (C. Hastings, "Approximations for
+// Digital Computers", 1955, sheet 43: the error function to 1.5e-7), so that a slope costs one exponential.
+__device__ __forceinline__ ff_act_pair ff_normal(float z)
+{
+    const float c = z != z ? z : fminf(fabsf(z), 20.f);              // the exponential is 0 in fp32 beyond
+    const float e = exp_neg(-0.5f * c * c), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, c, 1.f));
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float half = 0.5f * q * e;
+    return {z >= 0.f ? 1.f - half : half, e * 0.3989422804014327f};
+}
+
 template <int ACT> __device__ __forceinline__ float ff_act(float z)
 {
     if constexpr (ACT == SGNN_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-    else if constexpr (ACT == SGNN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    else if constexpr (ACT == SGNN_ACT_GELU) return z * ff_normal(z).f;
     else if constexpr (ACT == SGNN_ACT_GELU_TANH) return z * ff_logistic(ff_gelu_inner(z));
     else if constexpr (ACT == SGNN_ACT_SILU) return z * ff_logistic(z);
     else return z;
@@ -36,9 +47,9 @@ template <int ACT> __device__ __forceinline__ ff_act_pair ff_act_both(float z)
 {
     if constexpr (ACT == SGNN_ACT_RELU) return {ff_act<ACT>(z), z > 0.f ? 1.f : (z != z ? z : 0.f)};
     else if constexpr (ACT == SGNN_ACT_GELU) {
-        const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-        const float c = z != z ? z : fminf(fmaxf(z, -20.f), 20.f);       // the density is 0 in fp32 beyond
-        return {z * p, fmaf(c * 0.3989422804014327f, exp_neg(-0.5f * c * c), p)};
+        const ff_act_pair n = ff_normal(z);
+        const float c = z != z ? z : fminf(fmaxf(z, -20.f), 20.f);
+        return {z * n.f, fmaf(c, n.d, n.f)};
     } else if constexpr (ACT == SGNN_ACT_GELU_TANH) {
         const float s = ff_logistic(ff_gelu_inner(z));
         const float c = z != z ? z : fminf(fmaxf(z, -12.f), 12.f);

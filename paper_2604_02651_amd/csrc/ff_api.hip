@@ -167,13 +167,17 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (M == 0) return no_rows(ctx, n, dW, db, N, st);
     ws_alloc ws(ctx);
-    // [D0 | D1] in one matrix, each padded with zeros to whole 16-byte chunks
-    const int64_t np = ff_pad8(N), ldd = n * np;
-    void *D = b16 ? static_cast<void *>(ws.get<u16>((size_t)M * ldd)) : static_cast<void *>(ws.get<float>((size_t)M * ldd));
+    // [D0 | D1] in one matrix, each padded with zeros to whole 16-byte chunks; without an activation dY itself, if the products can read it
+    const bool is_dy = !need_z && (!b16 || (is16(dY) && ff_chunked(dY->ptr, N, dY->ld)));
+    const int64_t np = is_dy ? N : ff_pad8(N), ldd = is_dy ? dY->ld : n * np;
+    void *D = is_dy ? dY->ptr : (b16 ? static_cast<void *>(ws.get<u16>((size_t)M * ldd)) : static_cast<void *>(ws.get<float>((size_t)M * ldd)));
     if (!ws.ok) return no_scratch(ctx, name);
     const ff_mat d0 = {D, ldd, b16}, d1 = {b16 ? static_cast<void *>(static_cast<u16 *>(D) + np) : static_cast<void *>(static_cast<float *>(D) + np), ldd, b16};
     const ff_mat z0 = need_z ? view(Z[0]) : view(dY), z1 = n == 2 ? view(Z[1]) : ff_mat{};
-    const ff_mat *zp = n == 2 ? &z1 : nullptr, *dp = n == 2 ? &d1 : nullptr;
+    auto gradients = [&]() -> int {
+        if (is_dy && !any_db) return SGNN_OK;
+        return sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, n == 2 ? &z1 : nullptr, is_dy ? ff_mat{nullptr, 0, b16} : d0, n == 2 ? &d1 : nullptr, db, &ws, st);
+    };
     const bool few = dX && M <= sgnn_ff_rows_max(K, n * N);
     // the gradient of a few rows
     auto few_rows = [&]() -> int {
@@ -193,7 +197,7 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     };
     ff_op x, w[2];
     if (b16) {
-        rc = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, zp, d0, dp, db, &ws, st);
+        rc = gradients();
         if (rc) return rc;
         bool dx_done = false;
         if (few) {
@@ -202,6 +206,23 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
             dx_done = rc == SGNN_OK;
         }
         const ff_op d[2] = {{static_cast<const u16 *>(d0.p), ldd, 0}, {static_cast<const u16 *>(d1.p), ldd, 0}};
+        // both products of many rows onto up to 256 columns in one pass over X and D (gemm_bwd.hip), which reads fp32 weights and writes an fp32 gradient
+        if (n == 1 && dX && dW[0] && !dx_done && is16(X) && is16(dX)) {
+            const size_t off = ws.off;
+            const bool w32 = !is16(W[0]), direct = !is16(dW[0]) && dW[0]->ld == N;
+            float *wf = w32 ? static_cast<float *>(W[0]->ptr) : (K <= 256 && N <= 256 ? ws.get<float>((size_t)K * N) : nullptr);
+            float *cf = direct ? static_cast<float *>(dW[0]->ptr) : (K <= 256 && N <= 256 ? ws.get<float>((size_t)K * N) : nullptr);
+            if (wf && cf && ws.ok) {
+                // the weights are widened first: whether the kernel takes the call is known when it has been launched
+                if (!w32 && M >= 8192 && K > 64) rc = sgnn_launch_ff_convert(ctx, view(W[0]), K, N, ff_mat{wf, N, 0}, st);
+                if (rc) return rc;
+                rc = sgnn_launch_gemm_bwd(ctx, K, N, M, X->ptr, X->ld, D, ldd, wf, w32 ? W[0]->ld : N, dX->ptr, dX->ld, false, false, cf, nullptr, &ws, st);
+                if (rc == SGNN_OK) return direct ? SGNN_OK : sgnn_launch_ff_convert(ctx, ff_mat{cf, N, 0}, K, N, view(dW[0]), st);
+                if (rc != SGNN_ERR_UNSUPPORTED) return rc;
+            }
+            ws.off = off;
+            ws.ok = true;
+        }
         if (any_dw) {
             const size_t off = ws.off;
             rc = operand(ctx, name, X, false, &ws, st, &x);
@@ -232,7 +253,7 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
             x = parts_op(&ws, M, K);
             ex_x = ws.get<int32_t>((size_t)M);
         }
-        d[0] = d[1] = parts_op(&ws, M, ldd);
+        d[0] = d[1] = parts_op(&ws, M, n * np);
         d[1].p += np;
         ex_d = ws.get<int32_t>((size_t)M);
         if (any_dw) job[jobs++] = ff_parts{scan(X), words.key, ex_d, words.ex + 1, const_cast<u16 *>(x.p), x.ld, x.plane};
@@ -246,11 +267,11 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
         if (rc) return rc;
     }
     auto run = [&]() -> int {
-        int r = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, zp, d0, dp, db, &ws, st);
+        int r = gradients();
         if (!r && few) r = few_rows();
         if (r || !split) return r;
         const ff_row_parts xr = {scan(X), nullptr, 0, 0, ex_x, nullptr, nullptr};
-        const ff_row_parts dr = {{static_cast<const float *>(D), M, ldd, ldd}, const_cast<u16 *>(d[0].p), d[0].ld, d[0].plane, ex_d, ex_x, any_dw ? words.key : nullptr};
+        const ff_row_parts dr = {{static_cast<const float *>(D), M, n * np, ldd}, const_cast<u16 *>(d[0].p), d[0].ld, d[0].plane, ex_d, ex_x, any_dw ? words.key : nullptr};
         if (any_dw) r = sgnn_launch_ff_row_parts(ctx, xr, 0, nullptr, nullptr, st);
         if (!r) r = sgnn_launch_ff_row_parts(ctx, dr, nw, wscan, words.largest, st);
         if (!r) r = sgnn_launch_ff_parts(ctx, jobs, job, st);

@@ -70,7 +70,7 @@ template <int T, int V, bool GATED> __global__ __launch_bounds__(256) void ff_ac
                 s0[i] += d0[i];
                 s1[i] += d1[i];
             }
-            ff_store<T, V>(d0, a.D0, row, col, a.pcols - col);
+            if (a.D0.p) ff_store<T, V>(d0, a.D0, row, col, a.pcols - col);
             if (GATED) ff_store<T, V>(d1, a.D1, row, col, a.pcols - col);
         }
     }
@@ -122,6 +122,19 @@ template <int T> __global__ __launch_bounds__(256) void ff_pack_kernel(ff_mat sr
         float v[8];
         ff_load<T, 8>(v, src, row, col, cols - col);
         ff_store<FF_T16, 8>(v, dst, row, col, 8);
+    }
+}
+
+__global__ __launch_bounds__(256) void ff_convert_kernel(ff_mat src, int64_t rows, int cols, ff_mat dst)
+{
+    const int chunks = (cols + 7) / 8;
+    const int64_t n = rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / chunks;
+        const int col = 8 * (int)(i % chunks);
+        float v[8];
+        ff_load<FF_TANY, 8>(v, src, row, col, cols - col);
+        ff_store<FF_TANY, 8>(v, dst, row, col, cols - col);
     }
 }
 
@@ -284,6 +297,12 @@ int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t 
     const dim3 grid(flat_blocks(rows * (pcols / 8)));
     if (src.b16) SGNN_LAUNCH(ctx, st, "ff_pack_kernel", SGNN_TAG, ff_pack_kernel<FF_T16>, grid, dim3(256), 0, st, src, rows, (int)cols, (int)pcols, d);
     else SGNN_LAUNCH(ctx, st, "ff_pack_kernel", SGNN_TAG, ff_pack_kernel<FF_T32>, grid, dim3(256), 0, st, src, rows, (int)cols, (int)pcols, d);
+    return SGNN_OK;
+}
+
+int sgnn_launch_ff_convert(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, const ff_mat &dst, hipStream_t st)
+{
+    SGNN_LAUNCH(ctx, st, "ff_convert_kernel", SGNN_TAG, ff_convert_kernel, dim3(flat_blocks(rows * ((cols + 7) / 8))), dim3(256), 0, st, src, rows, (int)cols, dst);
     return SGNN_OK;
 }
 

@@ -462,11 +462,12 @@ int sgnn_launch_ff_nt(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
     return rc;
 }
 
-// Scratch of the products: partial results of tn (at most 64 ranges of M x N, or 768 tiles of 256 x 256 over all of them), sums of split tiles (512 of 64 x 128 and those
-// that made them up to 256)
+// Scratch of the products: partial results of tn (at most 512 ranges; over all of them 256 tiles of 256 x 256, or as many elements in others, or one result),
+// sums of split tiles (512 of 64 x 128)
 size_t sgnn_ff_gemm_ws_bytes(uint64_t d_in, uint64_t d_out)
 {
-    return std::max<uint64_t>(std::min<uint64_t>(2 * 64 * d_in * d_out, std::max<uint64_t>(768ull * 65536, 2 * d_in * d_out)) * 4, 768ull * 64 * 128 * 4) + 512;
+    const uint64_t results = 2 * d_in * d_out;
+    return std::max<uint64_t>(std::min<uint64_t>(512 * results, std::max<uint64_t>(256ull * 65536, results)), 512ull * 64 * 128) * 4 + 512;
 }
 
 int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
@@ -482,7 +483,7 @@ int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
     const int64_t slices = cdiv(K, bk);
     // the widest tile that leaves a range of eight slices and more to a workgroup a compute unit
     auto tiles = [&](int64_t bm, int64_t bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn) * mats; };
-    auto ranges = [&](int64_t n, int64_t total) { return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, slices / 4), total / n)); };
+    auto ranges = [&](int64_t n, int64_t total) { return std::max<int64_t>(1, std::min<int64_t>(slices / 4, total / n)); };
     int tile = FFT_SMALL;
     int64_t n = tiles(64, 128), splits = ranges(n, 512);
     const int64_t nw = pl == 1 ? tiles(256, 256) : tiles(256, 128), nm = tiles(128, 128);
