@@ -103,9 +103,9 @@ struct ff_epilogue {
     const float *bias[2];             // of each projection, or null
     ff_mat R, Y, Z[2];                // residual, result, pre-activations kept (p may be null but for Y)
 };
-// an operand, chunked (ff_chunked): bfloat16 (pl = 1), or two planes of fp16 parts `plane` elements apart (pl = 2: fp32).  ex_rows, ex: the scales of the
+// an operand, chunked (ff_chunked): bfloat16 (pl = 1), or fp16 parts (pl = 2: fp32), eight first ones and eight second ones in turn.  ex_rows, ex: the scales of the
 // rows of A, if they have their own, and of everything else (of both operands together)
-struct ff_op { const u16 *p; int64_t ld, plane; };
+struct ff_op { const u16 *p; int64_t ld; };        // ld in elements of 16 bits
 // Y = act(A B + bias) + R, with mats = 2 Y = act(A B0 + bias0) * (A B1 + bias1); A [M x K], B [K x N]; the epilogue's matrices as they come
 int sgnn_launch_ff_nn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
                       const ff_epilogue &e, ws_alloc *ws, hipStream_t st);
@@ -129,17 +129,17 @@ size_t sgnn_ff_rows_ws_bytes();
 int sgnn_launch_ff_pack(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, u16 *dst, int64_t ldd, hipStream_t st);
 // dst = src in dst's storage
 int sgnn_launch_ff_convert(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64_t cols, const ff_mat &dst, hipStream_t st);
-// fp32 operands as two planes of fp16 parts [rows x ff_pad8(cols)], zeros behind the last column (ff_gemm.hip says how and why).
+// fp32 operands as fp16 parts [rows x 2 ff_pad8(cols)], zeros behind the last column (ff_gemm.hip says how and why).
 struct ff_scan { const float *p; int64_t rows, cols, ld; };
 // The rows of one matrix, each scaled by a power of two of its own: 2^ex[row] takes the row's largest finite magnitude to [2^14, 2^15); FF_EX_ZERO
 // for a row without one.  to null: the exponents only.  With `other`, the exponents of another matrix' rows, *key = max(*key, FF_EX_KEY - ex[row] -
 // other[row]).  The same launch finds the largest finite magnitude of up to two weight matrices, *word = max(*word, its bits).
-struct ff_row_parts { ff_scan m; u16 *to; int64_t ld, plane; int32_t *ex; const int32_t *other; uint32_t *key; };
+struct ff_row_parts { ff_scan m; u16 *to; int64_t ld; int32_t *ex; const int32_t *other; uint32_t *key; };
 constexpr int FF_EX_ZERO = 2000, FF_EX_KEY = 8192;
 int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *word, hipStream_t st);
 // Up to three matrices with the scale known: rows == null, one for the matrix, from the largest magnitude in *word; else FF_EX_KEY - *word - rows[row] for
 // each row.  *ex: the scale of the matrix, or FF_EX_KEY - *word
-struct ff_parts { ff_scan m; const uint32_t *word; const int32_t *rows; int32_t *ex; u16 *to; int64_t ld, plane; };
+struct ff_parts { ff_scan m; const uint32_t *word; const int32_t *rows; int32_t *ex; u16 *to; int64_t ld; };
 int sgnn_launch_ff_parts(sgnn_ctx *ctx, int n, const ff_parts *m, hipStream_t st);
 // (D0 without memory: the column sums only)
 // D0 = dY * act'(Z0), or with Z1 D0 = dY * Z1 * act'(Z0) and D1 = dY * act(Z0); zeros in the columns from cols to pcols; column sums (before

@@ -37,13 +37,13 @@ int no_scratch(sgnn_ctx *ctx, const char *name) { return sgnn_fail(ctx, SGNN_ERR
 int operand(sgnn_ctx *ctx, const char *name, const sgnn_mat *m, bool pack, ws_alloc *ws, hipStream_t st, ff_op *op)
 {
     if (!pack && m->dtype == SGNN_BF16 && ff_chunked(m->ptr, m->cols, m->ld)) {
-        *op = ff_op{static_cast<const u16 *>(m->ptr), m->ld, 0};
+        *op = ff_op{static_cast<const u16 *>(m->ptr), m->ld};
         return SGNN_OK;
     }
     const int64_t ld = ff_pad8(m->cols);
     u16 *to = ws->get<u16>((size_t)m->rows * ld);
     if (!ws->ok) return no_scratch(ctx, name);
-    *op = ff_op{to, ld, 0};
+    *op = ff_op{to, ld};
     return sgnn_launch_ff_pack(ctx, view(m), m->rows, m->cols, to, ld, st);
 }
 
@@ -52,8 +52,8 @@ ff_scan scan(const sgnn_mat *m) { return ff_scan{static_cast<const float *>(m->p
 // scratch for the parts of an fp32 matrix
 ff_op parts_op(ws_alloc *ws, int64_t rows, int64_t cols)
 {
-    const int64_t ld = ff_pad8(cols);
-    return ff_op{ws->get<u16>((size_t)2 * rows * ld), ld, rows * ld};
+    const int64_t ld = 2 * ff_pad8(cols);
+    return ff_op{ws->get<u16>((size_t)rows * ld), ld};
 }
 
 // zeros for the gradients of weights and biases of a batch without rows
@@ -126,13 +126,13 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
     for (int q = 0; q < n; ++q) {
         w[q] = parts_op(&ws, K, N);
         ws_[q] = scan(W[q]);
-        wp[q] = ff_parts{ws_[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld, w[q].plane};
+        wp[q] = ff_parts{ws_[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld};
     }
     if (!ws.ok) return no_scratch(ctx, name);
     rc = sgnn_ff_open(ctx, st);
     if (rc) return rc;
     auto run = [&]() -> int {
-        const ff_row_parts xr = {scan(X), const_cast<u16 *>(x.p), x.ld, x.plane, ex_rows, nullptr, nullptr};
+        const ff_row_parts xr = {scan(X), const_cast<u16 *>(x.p), x.ld, ex_rows, nullptr, nullptr};
         int r = sgnn_launch_ff_row_parts(ctx, xr, n, ws_, words.largest, st);
         if (!r) r = sgnn_launch_ff_parts(ctx, n, wp, st);
         return r ? r : sgnn_launch_ff_nn(ctx, 2, M, N, K, n, x, w, ex_rows, words.ex, e, &ws, st);
@@ -205,7 +205,7 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
             if (rc != SGNN_OK && rc != SGNN_ERR_UNSUPPORTED) return rc;
             dx_done = rc == SGNN_OK;
         }
-        const ff_op d[2] = {{static_cast<const u16 *>(d0.p), ldd, 0}, {static_cast<const u16 *>(d1.p), ldd, 0}};
+        const ff_op d[2] = {{static_cast<const u16 *>(d0.p), ldd}, {static_cast<const u16 *>(d1.p), ldd}};
         // both products of many rows onto up to 256 columns in one pass over X and D (gemm_bwd.hip), which reads fp32 weights and writes an fp32 gradient
         if (n == 1 && dX && dW[0] && !dx_done && is16(X) && is16(dX)) {
             const size_t off = ws.off;
@@ -254,13 +254,13 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
             ex_x = ws.get<int32_t>((size_t)M);
         }
         d[0] = d[1] = parts_op(&ws, M, n * np);
-        d[1].p += np;
+        d[1].p += 2 * np;
         ex_d = ws.get<int32_t>((size_t)M);
-        if (any_dw) job[jobs++] = ff_parts{scan(X), words.key, ex_d, words.ex + 1, const_cast<u16 *>(x.p), x.ld, x.plane};
+        if (any_dw) job[jobs++] = ff_parts{scan(X), words.key, ex_d, words.ex + 1, const_cast<u16 *>(x.p), x.ld};
         for (int q = 0; q < n && tiles_dx; ++q) {
             w[q] = parts_op(&ws, K, N);
             wscan[nw++] = scan(W[q]);
-            job[jobs++] = ff_parts{wscan[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld, w[q].plane};
+            job[jobs++] = ff_parts{wscan[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld};
         }
         if (!ws.ok) return no_scratch(ctx, name);
         rc = sgnn_ff_open(ctx, st);
@@ -270,8 +270,8 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
         int r = gradients();
         if (!r && few) r = few_rows();
         if (r || !split) return r;
-        const ff_row_parts xr = {scan(X), nullptr, 0, 0, ex_x, nullptr, nullptr};
-        const ff_row_parts dr = {{static_cast<const float *>(D), M, n * np, ldd}, const_cast<u16 *>(d[0].p), d[0].ld, d[0].plane, ex_d, ex_x, any_dw ? words.key : nullptr};
+        const ff_row_parts xr = {scan(X), nullptr, 0, ex_x, nullptr, nullptr};
+        const ff_row_parts dr = {{static_cast<const float *>(D), M, n * np, ldd}, const_cast<u16 *>(d[0].p), d[0].ld, ex_d, ex_x, any_dw ? words.key : nullptr};
         if (any_dw) r = sgnn_launch_ff_row_parts(ctx, xr, 0, nullptr, nullptr, st);
         if (!r) r = sgnn_launch_ff_row_parts(ctx, dr, nw, wscan, words.largest, st);
         if (!r) r = sgnn_launch_ff_parts(ctx, jobs, job, st);

@@ -150,8 +150,8 @@ template <int V, class F> __device__ __forceinline__ void for_chunks(int64_t row
 
 __device__ __forceinline__ int exponent_of(uint32_t bits, int none) { return bits ? 14 + 127 - (int)(bits >> 23) : none; }
 
-// eight values times 2^ex as their parts
-__device__ __forceinline__ void store_parts(const float (&v)[8], int ex, u16 *to, int64_t plane)
+// eight values times 2^ex as their parts: the eight first ones, then the eight second ones
+__device__ __forceinline__ void store_parts(const float (&v)[8], int ex, u16 *to)
 {
     _Float16 h[2][8];
 #pragma unroll
@@ -162,7 +162,7 @@ __device__ __forceinline__ void store_parts(const float (&v)[8], int ex, u16 *to
         h[1][e] = (_Float16)(fabsf(x) < __builtin_inff() ? r : 0.f);
     }
 #pragma unroll
-    for (int q = 0; q < 2; ++q) *reinterpret_cast<u32x4 *>(to + q * plane) = *reinterpret_cast<const u32x4 *>(h[q]);
+    for (int q = 0; q < 2; ++q) *reinterpret_cast<u32x4 *>(to + 8 * q) = *reinterpret_cast<const u32x4 *>(h[q]);
 }
 
 struct ffe_rows { ff_row_parts r; ff_scan w[2]; uint32_t *word; };
@@ -214,7 +214,7 @@ template <int G, int CH> __global__ __launch_bounds__(256) void ff_row_parts_ker
         if (p.to)
             each([&](float (&x)[8], int64_t col) {
                 if constexpr (CH == 0) load(x, col);
-                store_parts(x, ex, p.to + row * p.ld + col, p.plane);
+                store_parts(x, ex, p.to + row * p.ld + 2 * col);
             });
     }
     if (p.key) block_max((uint32_t)key, p.key);
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256) void ff_parts_kernel(ffe_parts s)
     for_chunks<8>(p.m.rows, p.m.cols, [&](int64_t row, int64_t col) {
         float v[8];
         ff_load<FF_T32, 8>(v, src, row, col, (int)min(p.m.cols - col, (int64_t)8));
-        store_parts(v, p.rows ? ex - p.rows[row] : ex, p.to + row * p.ld + col, p.plane);
+        store_parts(v, p.rows ? ex - p.rows[row] : ex, p.to + row * p.ld + 2 * col);
     });
 }
 

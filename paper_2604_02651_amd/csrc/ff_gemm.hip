@@ -49,27 +49,28 @@ struct ffg_args {
     uint32_t *clear;                  // two words that the next call wants at zero, or null
 };
 
-// Operand of R rows (or columns) by BK reduction steps in LDS
-template <int R, int BK, bool TR> struct ffg_operand {
-    static constexpr int ROW = TR ? R * 2 : BK * 2, LINES = TR ? BK : R, CH = ROW / 16, BYTES = R * BK * 2;
-    // chunk c of line l is at c ^ swizzle(l)
+// Operand of R rows (or columns) by BK reduction steps in LDS.  PL = 2: the 16-byte chunks of the two parts alternate in a row.
+template <int PL, int R, int BK, bool TR> struct ffg_operand {
+    static constexpr int ROW = (TR ? R : BK) * 2 * PL, CH = ROW / 16, BYTES = R * BK * 2 * PL;
+    // Chunk c of line l is at c ^ swizzle(l): what is read together, chunks of 32 bytes (of one part: every other 16) of four rows with transposing reads, one chunk of
+    // sixteen rows without, lies in different banks of the 256 bytes.
     static __device__ __forceinline__ int swizzle(int l)
     {
-        if constexpr (TR) return R >= 128 ? 4 * (l & 3) : 4 * ((l >> 1) & 1);
-        else return BK == 64 ? (l >> 1) & 7 : (l >> 2) & 3;
+        if constexpr (TR) return PL == 2 ? (l & 1) | ((l >> 1) & 1) << 3 : (R >= 128 ? 4 * (l & 3) : 4 * ((l >> 1) & 1));
+        else return ROW == 128 ? (l >> 1) & 7 : (l >> 2) & 3;
     }
 };
 
-// PL: 1 bfloat16, 2 fp32 as two planes of fp16 parts
+// PL: 1 bfloat16, 2 fp32 as two fp16 parts
 template <int PL, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR, int KIND>
 __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void ff_gemm_kernel(ffg_args a)
 {
     // gated: the tile's columns are half of B0's, half of B1's, each an operand of its own in LDS
     constexpr int PARTS = KIND == FFK_GLU ? 2 : 1, BNP = BN / PARTS;
-    using OA = ffg_operand<BM, BK, ATR>;
-    using OB = ffg_operand<BNP, BK, BTR>;
-    // a slice in LDS: the planes of A, then for each part the planes of B; loads of 1 KB (a wavefront's), load l of the slice by wavefront l % NW
-    constexpr int NW = WM * WN, TM = BM / 32 / WM, TN = BN / 32 / WN, STAGE = PL * (OA::BYTES + PARTS * OB::BYTES);
+    using OA = ffg_operand<PL, BM, BK, ATR>;
+    using OB = ffg_operand<PL, BNP, BK, BTR>;
+    // a slice in LDS: A, then B, or the tile's columns of both; loads of 1 KB (a wavefront's), load l of the slice by wavefront l % NW
+    constexpr int NW = WM * WN, TM = BM / 32 / WM, TN = BN / 32 / WN, STAGE = OA::BYTES + PARTS * OB::BYTES;
     constexpr int AL = OA::BYTES / 1024, BL = OB::BYTES / 1024, LOADS = STAGE / 1024 / NW;
     constexpr bool EVEN = AL % NW == 0 && BL % NW == 0;         // which operand a load is of does not depend on the wavefront
     static_assert(OA::BYTES % 1024 == 0 && OB::BYTES % 1024 == 0 && STAGE % (1024 * NW) == 0, "whole loads, as many for every wavefront");
@@ -92,13 +93,13 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
     const int s0 = (int)z * a.per_split, nslices = min(a.slices - s0, a.per_split), seg_slices = (int)((a.K + BK - 1) / BK);
 
     // load j of the wavefront: of which part of the slice, and the lane's place in it
-    struct place { bool b; int sub, line, chunk; };
+    struct place { bool b; int q, line, chunk; };
     auto where = [&](int j) {
         const int l = (EVEN ? 0 : wave) + NW * j;
         place p;
-        p.b = l >= PL * AL;
-        p.sub = p.b ? (l - PL * AL) / BL : l / AL;
-        const int at = ((p.b ? (l - PL * AL) % BL : l % AL) + (EVEN ? wave : 0)) * 64 + lane;
+        p.b = l >= AL;
+        p.q = p.b ? (l - AL) / BL : 0;
+        const int at = ((p.b ? (l - AL) % BL : l) + (EVEN ? wave : 0)) * 64 + lane;
         p.line = p.b ? at / OB::CH : at / OA::CH;
         p.chunk = p.b ? (at % OB::CH) ^ OB::swizzle(p.line) : (at % OA::CH) ^ OA::swizzle(p.line);
         return p;
@@ -108,8 +109,8 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
     for (int j = 0; j < LOADS; ++j) {
         const place p = where(j);
         const bool tr = p.b ? BTR : ATR;
-        const int64_t last = p.b ? a.N - 1 - n0 : a.M - 1 - m0, ld = p.b ? a.B[KIND == FFK_GLU ? p.sub / PL : 0].ld : a.A[0].ld;
-        off[j] = tr ? (uint32_t)p.line * (uint32_t)(2 * ld) + 16u * (uint32_t)min((int64_t)p.chunk, last / 8)
+        const int64_t last = p.b ? a.N - 1 - n0 : a.M - 1 - m0, ld = p.b ? a.B[KIND == FFK_GLU ? p.q : 0].ld : a.A[0].ld;
+        off[j] = tr ? (uint32_t)p.line * (uint32_t)(2 * ld) + 16u * (uint32_t)(PL * min((int64_t)(p.chunk / PL), last / 8) + p.chunk % PL)
                     : (uint32_t)min((int64_t)p.line, last) * (uint32_t)(2 * ld) + 16u * (uint32_t)p.chunk;
     }
     auto issue = [&](int s) {
@@ -118,18 +119,15 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
         const int64_t k0 = (int64_t)(sl - seg * seg_slices) * BK;
         unsigned char *stage = ffg_smem + (s % STAGES) * STAGE + 1024 * wave;
         const int left = (int)min(a.K - k0, (int64_t)BK);
-        const u16 *first_a = a.A[seg].p + (ATR ? k0 * a.A[0].ld + m0 : m0 * a.A[0].ld + k0);
+        const u16 *first_a = a.A[seg].p + (ATR ? k0 * a.A[0].ld + PL * m0 : m0 * a.A[0].ld + PL * k0);
         const u16 *first_b[PARTS];
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
             const int which = KIND == FFK_GLU ? q : (KIND == FFK_PARTIAL ? (int)mat : seg);
             const int64_t ld = a.B[KIND == FFK_GLU ? q : 0].ld;
-            first_b[q] = a.B[which].p + (BTR ? k0 * ld + n0 : (int64_t)n0 * ld + k0);
+            first_b[q] = a.B[which].p + (BTR ? k0 * ld + PL * n0 : (int64_t)n0 * ld + PL * k0);
         }
-        auto base = [&](const place &p) {
-            const int plane = PL > 1 ? p.sub % PL : 0, q = PARTS > 1 ? p.sub / PL : 0;
-            return reinterpret_cast<const unsigned char *>(p.b ? first_b[q] + plane * a.B[KIND == FFK_GLU ? q : 0].plane : first_a + plane * a.A[0].plane);
-        };
+        auto base = [&](const place &p) { return reinterpret_cast<const unsigned char *>(p.b ? first_b[PARTS > 1 ? p.q : 0] : first_a); };
         if (left >= BK) {
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) __builtin_amdgcn_global_load_lds(STREAM_GPTR(base(where(j)) + off[j]), STREAM_LPTR(stage + 1024 * NW * j), 16, 0, 0);
@@ -137,7 +135,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
                 const place p = where(j);
-                const unsigned char *g = ((p.b ? BTR : ATR) ? p.line : 8 * p.chunk) < left ? base(p) + off[j] : reinterpret_cast<const unsigned char *>(&ff_zeros);
+                const unsigned char *g = ((p.b ? BTR : ATR) ? p.line : 8 * (p.chunk / PL)) < left ? base(p) + off[j] : reinterpret_cast<const unsigned char *>(&ff_zeros);
                 __builtin_amdgcn_global_load_lds(STREAM_GPTR(g), STREAM_LPTR(stage + 1024 * NW * j), 16, 0, 0);
             }
         }
@@ -147,11 +145,11 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
     const int x = lane & 15, r3 = x >> 2, half = (lane >> 4) & 1;
     auto tr_at = [&](auto op, int blk) {
         using O = decltype(op);
-        return (8 * kh + r3) * O::ROW + ((blk * 4 + 2 * half + ((x & 3) >> 1)) ^ O::swizzle(r3)) * 16 + (x & 1) * 8;
+        return (8 * kh + r3) * O::ROW + ((PL * (blk * 4 + 2 * half + ((x & 3) >> 1))) ^ O::swizzle(r3)) * 16 + (x & 1) * 8;
     };
     auto kc_at = [&](auto op, int blk) {
         using O = decltype(op);
-        return (32 * blk + li) * O::ROW + ((kh ^ O::swizzle(li)) * 16);
+        return (32 * blk + li) * O::ROW + ((PL * kh) ^ O::swizzle(li)) * 16;
     };
     int at_a[TM], at_b[TN];
 #pragma unroll
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int blk = KIND == FFK_GLU ? wn * (TN / 2) + j % (TN / 2) : wn * TN + j;
-        at_b[j] = PL * OA::BYTES + (KIND == FFK_GLU ? j / (TN / 2) * PL * OB::BYTES : 0) + (BTR ? tr_at(OB(), blk) : kc_at(OB(), blk));
+        at_b[j] = OA::BYTES + (KIND == FFK_GLU ? j / (TN / 2) * OB::BYTES : 0) + (BTR ? tr_at(OB(), blk) : kc_at(OB(), blk));
     }
 
     f32x16 acc[TM][TN], low[PL > 1 ? TM : 1][PL > 1 ? TN : 1];
@@ -185,20 +183,21 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
 #pragma unroll
         for (int ks = 0; ks < BK / 16; ++ks) {
             u32x4 fa[PL][TM], fb[PL][TN];
-            auto fetch = [&](auto op, bool tr, int at) {
+            auto fetch = [&](auto op, bool tr, int at, int part) {
                 using O = decltype(op);
                 if (tr) {
+                    at ^= 16 * part;
                     const uint2 lo = read_tr(stage + at + 16 * ks * O::ROW), hi = read_tr(stage + at + (16 * ks + 4) * O::ROW);
                     return u32x4{lo.x, lo.y, hi.x, hi.y};
                 }
-                return read_row(stage + (at ^ (32 * ks)));
+                return read_row(stage + (at ^ (32 * PL * ks + 16 * part)));
             };
 #pragma unroll
             for (int p = 0; p < PL; ++p) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fb[p][j] = fetch(OB(), BTR, at_b[j] + p * OB::BYTES);
+                for (int j = 0; j < TN; ++j) fb[p][j] = fetch(OB(), BTR, at_b[j], p);
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fa[p][i] = fetch(OA(), ATR, at_a[i] + p * OA::BYTES);
+                for (int i = 0; i < TM; ++i) fa[p][i] = fetch(OA(), ATR, at_a[i], p);
             }
             auto multiply = [&](auto &c, int pa, int pb) {
 #pragma unroll
