@@ -284,23 +284,23 @@ template <int T, int V, int CH, int G> __global__ __launch_bounds__(threads<G>()
     out(2, sp);
 }
 
-// sum over the workgroups of partial[w][which][col], sixteen interleaved chains a column and then the chains in order
+// sum over the workgroups of partial[w][which][col]: 64 interleaved chains a column, sixteen columns a workgroup, and then the chains in order
 __global__ __launch_bounds__(1024) void block_norm_sums_kernel(const float *__restrict__ partial, int n, int d, float *__restrict__ o0, float *__restrict__ o1,
                                                                float *__restrict__ o2)
 {
     __shared__ float red[1024];
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6, j = blockIdx.x * 64 + tx;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j = blockIdx.x * 16 + tx;
     float s = 0.f;
     if (j < 3 * d) {
 #pragma unroll 8
-        for (int w = ty; w < n; w += 16) s += partial[(int64_t)w * 3 * d + j];
+        for (int w = ty; w < n; w += 64) s += partial[(int64_t)w * 3 * d + j];
     }
     red[threadIdx.x] = s;
     __syncthreads();
     if (ty == 0 && j < 3 * d) {
         float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) t += red[w * 64 + tx];
+#pragma unroll 16
+        for (int w = 0; w < 64; ++w) t += red[w * 16 + tx];
         float *o = j < d ? o0 : (j < 2 * d ? o1 : o2);
         if (o) o[j % d] = t;
     }
@@ -347,7 +347,7 @@ template <int T, int V> int launch_bwd(sgnn_ctx *ctx, const ff_norm &a, ws_alloc
         }
         SGNN_LAUNCH(ctx, st, "block_norm_bwd_kernel", SGNN_TAG, (block_norm_bwd_kernel<T, V, CH, G>), dim3(grid), dim3(threads<G>()), 0, st, a, partial);
         if (sums)
-            SGNN_LAUNCH(ctx, st, "block_norm_sums_kernel", SGNN_TAG, block_norm_sums_kernel, dim3(cdiv(3 * a.d, 64)), dim3(1024), 0, st, partial, (int)grid, a.d,
+            SGNN_LAUNCH(ctx, st, "block_norm_sums_kernel", SGNN_TAG, block_norm_sums_kernel, dim3(cdiv(3 * a.d, 16)), dim3(1024), 0, st, partial, (int)grid, a.d,
                         a.dgamma_post, a.dscale, a.dgamma_pre);
         return SGNN_OK;
     });

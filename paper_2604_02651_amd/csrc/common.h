@@ -39,11 +39,10 @@ struct sgnn_ctx {
 #define SGNN_PERSIST_STATUS_OFF (32768 - 256)
 #define SGNN_PERSIST_XENT_OFF 32768
 #define SGNN_PERSIST_XENT_BYTES (256 * 513 * 8)
-// Behind those what the feed-forward products leave at zero between calls: counts of arrivals (one a tile or column strip whose reduction is split) and two
-// maxima that give the scales of fp32 operands; and these scales.
+// Behind those the feed-forward products' counts of arrivals, one a tile or column strip whose reduction is split (zero between calls).
 #define SGNN_PERSIST_FFN_OFF (SGNN_PERSIST_XENT_OFF + SGNN_PERSIST_XENT_BYTES)
 #define SGNN_FFN_COUNTS 256
-#define SGNN_PERSIST_FFN_BYTES ((SGNN_FFN_COUNTS + 8) * 4)
+#define SGNN_PERSIST_FFN_BYTES (SGNN_FFN_COUNTS * 4)
 #define SGNN_PERSIST_BYTES (SGNN_PERSIST_FFN_OFF + SGNN_PERSIST_FFN_BYTES)
 
 // Areas of the persistent memory that are zero between calls: a call adds to them in one kernel and a later one of its kernels leaves zeros.

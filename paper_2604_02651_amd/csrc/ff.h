@@ -87,13 +87,8 @@ static inline bool ff_chunked(const void *p, int64_t cols, int64_t ld)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && cols % 8 == 0 && ld % 8 == 0 && ld <= (1 << 22);
 }
 
-// The context's words of these products: zero between calls (but for the exponents)
-struct ff_words { uint32_t *arrived, *key, *largest; int32_t *ex; };
-static inline ff_words sgnn_ff_words(sgnn_ctx *ctx)
-{
-    uint32_t *p = reinterpret_cast<uint32_t *>(ctx->persist + SGNN_PERSIST_FFN_OFF);
-    return {p, p + SGNN_FFN_COUNTS, p + SGNN_FFN_COUNTS + 1, reinterpret_cast<int32_t *>(p + SGNN_FFN_COUNTS + 4)};
-}
+// The context's counts of arrivals, zero between calls
+static inline uint32_t *sgnn_ff_arrived(sgnn_ctx *ctx) { return reinterpret_cast<uint32_t *>(ctx->persist + SGNN_PERSIST_FFN_OFF); }
 static inline int sgnn_ff_open(sgnn_ctx *ctx, hipStream_t st) { return sgnn_zero_open(ctx, SGNN_ZERO_FFN, ctx->persist + SGNN_PERSIST_FFN_OFF, SGNN_PERSIST_FFN_BYTES, st); }
 static inline int sgnn_ff_close(sgnn_ctx *ctx, int rc, hipStream_t st) { return sgnn_zero_close(ctx, rc, SGNN_ZERO_FFN, ctx->persist + SGNN_PERSIST_FFN_OFF, SGNN_PERSIST_FFN_BYTES, st); }
 
@@ -132,14 +127,17 @@ int sgnn_launch_ff_convert(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64
 // fp32 operands as fp16 parts [rows x 2 ff_pad8(cols)], zeros behind the last column (ff_gemm.hip says how and why).
 struct ff_scan { const float *p; int64_t rows, cols, ld; };
 // The rows of one matrix, each scaled by a power of two of its own: 2^ex[row] takes the row's largest finite magnitude to [2^14, 2^15); FF_EX_ZERO
-// for a row without one.  to null: the exponents only.  With `other`, the exponents of another matrix' rows, *key = max(*key, FF_EX_KEY - ex[row] -
-// other[row]).  The same launch finds the largest finite magnitude of up to two weight matrices, *word = max(*word, its bits).
+// for a row without one.  to null: the exponents only.  With `other`, the exponents of another matrix' rows, every workgroup (sgnn_ff_row_groups of them)
+// leaves the largest FF_EX_KEY - ex[row] - other[row] of its rows in a word of key.  The same launch finds the largest finite magnitudes of up to two weight
+// matrices: a word of largest, its bits, for every workgroup (sgnn_ff_scan_groups for each matrix).
 struct ff_row_parts { ff_scan m; u16 *to; int64_t ld; int32_t *ex; const int32_t *other; uint32_t *key; };
-constexpr int FF_EX_ZERO = 2000, FF_EX_KEY = 8192;
-int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *word, hipStream_t st);
-// Up to three matrices with the scale known: rows == null, one for the matrix, from the largest magnitude in *word; else FF_EX_KEY - *word - rows[row] for
-// each row.  *ex: the scale of the matrix, or FF_EX_KEY - *word
-struct ff_parts { ff_scan m; const uint32_t *word; const int32_t *rows; int32_t *ex; u16 *to; int64_t ld; };
+constexpr int FF_EX_ZERO = 2000, FF_EX_KEY = 8192, FF_ROW_WORDS = 4096, FF_SCAN_WORDS = 512;
+unsigned sgnn_ff_row_groups(int64_t rows, int64_t cols);
+unsigned sgnn_ff_scan_groups(int n, const ff_scan *w);
+int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *largest, hipStream_t st);
+// Up to three matrices with the scale known from such words: rows == null, one scale for the matrix; else FF_EX_KEY - largest word - rows[row] for
+// each row.  *ex: the scale of the matrix, or FF_EX_KEY - largest word
+struct ff_parts { ff_scan m; const uint32_t *word; int words; const int32_t *rows; int32_t *ex; u16 *to; int64_t ld; };
 int sgnn_launch_ff_parts(sgnn_ctx *ctx, int n, const ff_parts *m, hipStream_t st);
 // (D0 without memory: the column sums only)
 // D0 = dY * act'(Z0), or with Z1 D0 = dY * Z1 * act'(Z0) and D1 = dY * act(Z0); zeros in the columns from cols to pcols; column sums (before

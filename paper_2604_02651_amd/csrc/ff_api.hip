@@ -118,26 +118,22 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
         if (rc) return rc;
         return sgnn_launch_ff_nn(ctx, 1, M, N, K, n, x, w, nullptr, nullptr, e, &ws, st);
     }
-    const ff_words words = sgnn_ff_words(ctx);
-    ff_scan ws_[2];
-    ff_parts wp[2];
+    // fp32: the rows of X scaled by themselves, the weights by their largest value (ff_gemm.hip)
+    ff_scan scans[2];
+    ff_parts job[2];
     x = parts_op(&ws, M, K);
-    int32_t *const ex_rows = ws.get<int32_t>((size_t)M);
+    int32_t *const ex_rows = ws.get<int32_t>((size_t)M + 1), *const ex = ex_rows + M;
+    uint32_t *const largest = ws.get<uint32_t>(2 * FF_SCAN_WORDS);
     for (int q = 0; q < n; ++q) {
         w[q] = parts_op(&ws, K, N);
-        ws_[q] = scan(W[q]);
-        wp[q] = ff_parts{ws_[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld};
+        scans[q] = scan(W[q]);
     }
     if (!ws.ok) return no_scratch(ctx, name);
-    rc = sgnn_ff_open(ctx, st);
-    if (rc) return rc;
-    auto run = [&]() -> int {
-        const ff_row_parts xr = {scan(X), const_cast<u16 *>(x.p), x.ld, ex_rows, nullptr, nullptr};
-        int r = sgnn_launch_ff_row_parts(ctx, xr, n, ws_, words.largest, st);
-        if (!r) r = sgnn_launch_ff_parts(ctx, n, wp, st);
-        return r ? r : sgnn_launch_ff_nn(ctx, 2, M, N, K, n, x, w, ex_rows, words.ex, e, &ws, st);
-    };
-    return sgnn_ff_close(ctx, run(), st);
+    const int words = n * (int)sgnn_ff_scan_groups(n, scans);
+    for (int q = 0; q < n; ++q) job[q] = ff_parts{scans[q], largest, words, nullptr, ex, const_cast<u16 *>(w[q].p), w[q].ld};
+    rc = sgnn_launch_ff_row_parts(ctx, ff_row_parts{scan(X), const_cast<u16 *>(x.p), x.ld, ex_rows, nullptr, nullptr}, n, scans, largest, st);
+    if (!rc) rc = sgnn_launch_ff_parts(ctx, n, job, st);
+    return rc ? rc : sgnn_launch_ff_nn(ctx, 2, M, N, K, n, x, w, ex_rows, ex, e, &ws, st);
 }
 
 // Backward of either: D = the gradients of the pre-activations, then the products
@@ -242,44 +238,37 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     }
     // fp32: the gradients' rows are scaled by themselves, the rows of X so that with the gradients' all products have one scale (ff_gemm.hip)
     const bool tiles_dx = dX && !few, split = any_dw || tiles_dx;
-    const ff_words words = sgnn_ff_words(ctx);
+    rc = gradients();
+    if (!rc && few) rc = few_rows();
+    if (rc || !split) return rc;
     ff_op d[2];
     ff_parts job[3];
-    ff_scan wscan[2];
+    ff_scan scans[2];
     int jobs = 0, nw = 0;
-    int32_t *ex_x = nullptr, *ex_d = nullptr;
-    if (split) {
-        if (any_dw) {
-            x = parts_op(&ws, M, K);
-            ex_x = ws.get<int32_t>((size_t)M);
-        }
-        d[0] = d[1] = parts_op(&ws, M, n * np);
-        d[1].p += 2 * np;
-        ex_d = ws.get<int32_t>((size_t)M);
-        if (any_dw) job[jobs++] = ff_parts{scan(X), words.key, ex_d, words.ex + 1, const_cast<u16 *>(x.p), x.ld};
-        for (int q = 0; q < n && tiles_dx; ++q) {
-            w[q] = parts_op(&ws, K, N);
-            wscan[nw++] = scan(W[q]);
-            job[jobs++] = ff_parts{wscan[q], words.largest, nullptr, words.ex, const_cast<u16 *>(w[q].p), w[q].ld};
-        }
-        if (!ws.ok) return no_scratch(ctx, name);
-        rc = sgnn_ff_open(ctx, st);
-        if (rc) return rc;
+    int32_t *const ex_d = ws.get<int32_t>((size_t)M + 2), *const ex = ex_d + M;          // of the rows of D; of the weights, and of x d
+    int32_t *ex_x = nullptr;
+    uint32_t *const largest = ws.get<uint32_t>(2 * FF_SCAN_WORDS + FF_ROW_WORDS), *const key = largest + 2 * FF_SCAN_WORDS;
+    d[0] = d[1] = parts_op(&ws, M, n * np);
+    d[1].p += 2 * np;
+    if (any_dw) {
+        x = parts_op(&ws, M, K);
+        ex_x = ws.get<int32_t>((size_t)M);
+        job[jobs++] = ff_parts{scan(X), key, (int)sgnn_ff_row_groups(M, n * np), ex_d, ex + 1, const_cast<u16 *>(x.p), x.ld};
     }
-    auto run = [&]() -> int {
-        int r = gradients();
-        if (!r && few) r = few_rows();
-        if (r || !split) return r;
-        const ff_row_parts xr = {scan(X), nullptr, 0, ex_x, nullptr, nullptr};
-        const ff_row_parts dr = {{static_cast<const float *>(D), M, n * np, ldd}, const_cast<u16 *>(d[0].p), d[0].ld, ex_d, ex_x, any_dw ? words.key : nullptr};
-        if (any_dw) r = sgnn_launch_ff_row_parts(ctx, xr, 0, nullptr, nullptr, st);
-        if (!r) r = sgnn_launch_ff_row_parts(ctx, dr, nw, wscan, words.largest, st);
-        if (!r) r = sgnn_launch_ff_parts(ctx, jobs, job, st);
-        if (!r && any_dw) r = weights(2, x, d, nullptr, words.ex + 1);
-        if (!r && tiles_dx) r = sgnn_launch_ff_nt(ctx, 2, M, K, N, n, d, w, ex_d, words.ex, view(dX), &ws, st);
-        return r;
-    };
-    return split ? sgnn_ff_close(ctx, run(), st) : run();
+    for (; tiles_dx && nw < n; ++nw) {
+        w[nw] = parts_op(&ws, K, N);
+        scans[nw] = scan(W[nw]);
+    }
+    if (!ws.ok) return no_scratch(ctx, name);
+    const int words = nw * (int)sgnn_ff_scan_groups(nw, scans);
+    for (int q = 0; q < nw; ++q) job[jobs++] = ff_parts{scans[q], largest, words, nullptr, ex, const_cast<u16 *>(w[q].p), w[q].ld};
+    if (any_dw) rc = sgnn_launch_ff_row_parts(ctx, ff_row_parts{scan(X), nullptr, 0, ex_x, nullptr, nullptr}, 0, nullptr, nullptr, st);
+    const ff_scan ds = {static_cast<const float *>(D), M, n * np, ldd};
+    if (!rc) rc = sgnn_launch_ff_row_parts(ctx, ff_row_parts{ds, const_cast<u16 *>(d[0].p), d[0].ld, ex_d, ex_x, any_dw ? key : nullptr}, nw, scans, largest, st);
+    if (!rc) rc = sgnn_launch_ff_parts(ctx, jobs, job, st);
+    if (!rc && any_dw) rc = weights(2, x, d, nullptr, ex + 1);
+    if (!rc && tiles_dx) rc = sgnn_launch_ff_nt(ctx, 2, M, K, N, n, d, w, ex_d, ex, view(dX), &ws, st);
+    return rc;
 }
 
 } // namespace
@@ -294,7 +283,8 @@ int sgnn_ctx_reserve_ffn(sgnn_ctx *ctx, uint64_t rows, uint32_t d_in, uint32_t d
     if (rc) return rc;
     const uint64_t di = ff_pad8(d_in), dn = ff_pad8(d_out);
     // fp32: both gradients of the pre-activations and their parts, the parts of X and of both weights; bfloat16 needs less
-    size_t need = rows * (2 * dn * 8 + di * 4 + 8) + 2 * di * dn * 4 + std::max(sgnn_ff_gemm_ws_bytes(di, dn), sgnn_ff_rows_ws_bytes()) + sgnn_ff_sums_ws_bytes(dn) + 16 * 256;
+    size_t need = rows * (2 * dn * 8 + di * 4 + 8) + 2 * di * dn * 4 + std::max(sgnn_ff_gemm_ws_bytes(di, dn), sgnn_ff_rows_ws_bytes()) + sgnn_ff_sums_ws_bytes(dn) +
+                  (2 * FF_SCAN_WORDS + FF_ROW_WORDS) * 4 + 16 * 256;
     need = std::max(need, sgnn_block_norm_ws_bytes(std::max(d_in, d_out)));
     if (need > ctx->ws_bytes) {
         SGNN_HIP(ctx, hipDeviceSynchronize());

@@ -4,14 +4,13 @@
 //   row_parts, parts   an fp32 matrix as two planes of fp16 parts, scaled by powers of two (ff_gemm.hip says how and why): by one for each row from the
 //            row's largest magnitude, or by a given one
 //   pack     a matrix as the tile kernel takes it: bfloat16, rows padded with zeros to whole 16-byte chunks
-// A workgroup has a strip of 32 chunks of columns (16 bytes a lane, 512 a row) and eight rows at a time.  Column sums: a thread adds up its rows, the
-// eight rows of threads meet in LDS, every workgroup writes one partial sum a column, and a second kernel adds these in a fixed order.
+// A workgroup of act_bwd has a strip of CH chunks of columns (16 bytes a lane; 32 of them, or as few as hold a narrow matrix) and 256 / CH rows at a time.  Column
+// sums: a thread adds up its rows, the rows of threads meet in LDS, every workgroup writes one partial sum a column, and a second kernel adds these in
+// a fixed order.
 #include "ff.h"
 #include "ff_act.h"
 
 namespace {
-
-constexpr int FFE_CH = 32, FFE_ROWS = 8;
 
 struct ffe_args {
     int64_t rows;
@@ -28,22 +27,20 @@ __device__ __forceinline__ uint32_t finite_max(uint32_t m, float v)
     return b < 0x7f800000u ? max(m, b) : m;
 }
 
-// The workgroup's largest m into *word.  A workgroup that has nothing larger than what it reads leaves the word alone (2048 atomic operations on one
-// word would be the longest part of a small matrix).
-__device__ __forceinline__ void block_max(uint32_t m, uint32_t *word)
+// The workgroup's largest m (of 256 threads), in thread 0
+__device__ __forceinline__ uint32_t block_max(uint32_t m)
 {
     __shared__ uint32_t red[4];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    const uint32_t t = max(max(red[0], red[1]), max(red[2], red[3]));
-    if (t > __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) __hip_atomic_fetch_max(word, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return max(max(red[0], red[1]), max(red[2], red[3]));
 }
 
-template <int T, int V, bool GATED> __global__ __launch_bounds__(256) void ff_act_bwd_kernel(ffe_args a)
+template <int T, int V, bool GATED, int FFE_CH> __global__ __launch_bounds__(256) void ff_act_bwd_kernel(ffe_args a)
 {
+    constexpr int FFE_ROWS = 256 / FFE_CH;
     __shared__ float red[FFE_ROWS][FFE_CH * V];
     const int tx = threadIdx.x % FFE_CH, ty = threadIdx.x / FFE_CH;
     const int col = (blockIdx.x * FFE_CH + tx) * V, left = a.cols - col;
@@ -84,29 +81,29 @@ template <int T, int V, bool GATED> __global__ __launch_bounds__(256) void ff_ac
         const int j = threadIdx.x, c = blockIdx.x * FFE_CH * V + j;
         if (j < FFE_CH * V && c < a.cols) {
             float t = 0.f;
-#pragma unroll
+#pragma unroll 8
             for (int w = 0; w < FFE_ROWS; ++w) t += red[w][j];
             a.partial[((int64_t)blockIdx.y * (GATED ? 2 : 1) + q) * a.cols + c] = t;
         }
     }
 }
 
-// out[which][col] = sum over the workgroups of partial[w][which][col], sixteen interleaved chains a column and then the chains in order
+// out[which][col] = sum over the workgroups of partial[w][which][col]: 64 interleaved chains a column, sixteen columns a workgroup, and then the chains in order
 __global__ __launch_bounds__(1024) void ff_colsum_kernel(const float *__restrict__ partial, int n, int cols, int outs, float *__restrict__ o0, float *__restrict__ o1)
 {
     __shared__ float red[1024];
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6, j = blockIdx.x * 64 + tx;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j = blockIdx.x * 16 + tx;
     float s = 0.f;
     if (j < outs * cols) {
 #pragma unroll 8
-        for (int w = ty; w < n; w += 16) s += partial[(int64_t)w * outs * cols + j];
+        for (int w = ty; w < n; w += 64) s += partial[(int64_t)w * outs * cols + j];
     }
     red[threadIdx.x] = s;
     __syncthreads();
     if (ty == 0 && j < outs * cols) {
         float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) t += red[w * 64 + tx];
+#pragma unroll 16
+        for (int w = 0; w < 64; ++w) t += red[w * 16 + tx];
         float *o = j < cols ? o0 : o1;
         if (o) o[j < cols ? j : j - cols] = t;
     }
@@ -138,11 +135,11 @@ __global__ __launch_bounds__(256) void ff_convert_kernel(ff_mat src, int64_t row
     }
 }
 
-// f(row, first column) for the chunks of V columns of a matrix, dealt to the threads of gridDim.x workgroups
-template <int V, class F> __device__ __forceinline__ void for_chunks(int64_t rows, int64_t cols, F f)
+// f(row, first column) for the chunks of V columns of a matrix, dealt to the threads of `groups` workgroups
+template <int V, class F> __device__ __forceinline__ void for_chunks(int64_t rows, int64_t cols, unsigned groups, F f)
 {
     const int64_t chunks = (cols + V - 1) / V, n = rows * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)groups * 256) {
         const int64_t row = n <= 0xffffffffll ? (int64_t)((uint32_t)i / (uint32_t)chunks) : i / chunks;
         f(row, V * (i - row * chunks));
     }
@@ -165,30 +162,33 @@ __device__ __forceinline__ void store_parts(const float (&v)[8], int ex, u16 *to
     for (int q = 0; q < 2; ++q) *reinterpret_cast<u32x4 *>(to + 8 * q) = *reinterpret_cast<const u32x4 *>(h[q]);
 }
 
-struct ffe_rows { ff_row_parts r; ff_scan w[2]; uint32_t *word; };
+struct ffe_rows { ff_row_parts r; ff_scan w[2]; uint32_t *largest; int scans; };
 
 // G lanes a row; CH chunks of eight values a lane stay in registers, or (CH = 0) a row is read once for its largest magnitude and once for its parts
-template <int G, int CH> __global__ __launch_bounds__(256) void ff_row_parts_kernel(ffe_rows s)
+template <int G, int CH> __global__ __launch_bounds__(256) void ff_row_parts_kernel(ffe_rows s, unsigned groups)
 {
     if (blockIdx.y > 0) {
+        if ((int)blockIdx.x >= s.scans) return;
         const ff_scan &m = s.w[blockIdx.y - 1];
         const ff_mat src = {m.p, m.ld, 0};
         uint32_t largest = 0;
-        for_chunks<8>(m.rows, m.cols, [&](int64_t row, int64_t col) {
+        for_chunks<8>(m.rows, m.cols, s.scans, [&](int64_t row, int64_t col) {
             float v[8];
             ff_load<FF_T32, 8>(v, src, row, col, (int)min(m.cols - col, (int64_t)8));
 #pragma unroll
             for (int e = 0; e < 8; ++e) largest = finite_max(largest, v[e]);
         });
-        block_max(largest, s.word);
+        const uint32_t t = block_max(largest);
+        if (threadIdx.x == 0) s.largest[(blockIdx.y - 1) * s.scans + blockIdx.x] = t;
         return;
     }
+    if (blockIdx.x >= groups) return;
     const ff_row_parts &p = s.r;
     const ff_mat src = {p.m.p, p.m.ld, 0};
     const int l = threadIdx.x % G;
     const int64_t chunks = (p.m.cols + 7) / 8;
     int key = 0;
-    for (int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < p.m.rows; row += (int64_t)gridDim.x * (256 / G)) {
+    for (int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < p.m.rows; row += (int64_t)groups * (256 / G)) {
         float v[CH ? CH : 1][8];
         uint32_t largest = 0;
         auto each = [&](auto f) {
@@ -217,7 +217,10 @@ template <int G, int CH> __global__ __launch_bounds__(256) void ff_row_parts_ker
                 store_parts(x, ex, p.to + row * p.ld + 2 * col);
             });
     }
-    if (p.key) block_max((uint32_t)key, p.key);
+    if (p.key) {
+        const uint32_t t = block_max((uint32_t)key);
+        if (threadIdx.x == 0) p.key[blockIdx.x] = t;
+    }
 }
 
 struct ffe_parts { ff_parts m[3]; };
@@ -226,9 +229,12 @@ __global__ __launch_bounds__(256) void ff_parts_kernel(ffe_parts s)
 {
     const ff_parts &p = s.m[blockIdx.y];
     const ff_mat src = {p.m.p, p.m.ld, 0};
-    const int ex = p.rows ? FF_EX_KEY - (int)*p.word : exponent_of(*p.word, 0);
+    uint32_t largest = 0;
+    for (int i = threadIdx.x; i < p.words; i += 256) largest = max(largest, p.word[i]);
+    largest = block_max(largest);
+    const int ex = p.rows ? FF_EX_KEY - (int)largest : exponent_of(largest, 0);
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.ex = ex;
-    for_chunks<8>(p.m.rows, p.m.cols, [&](int64_t row, int64_t col) {
+    for_chunks<8>(p.m.rows, p.m.cols, gridDim.x, [&](int64_t row, int64_t col) {
         float v[8];
         ff_load<FF_T32, 8>(v, src, row, col, (int)min(p.m.cols - col, (int64_t)8));
         store_parts(v, p.rows ? ex - p.rows[row] : ex, p.to + row * p.ld + 2 * col);
@@ -241,9 +247,6 @@ __global__ __launch_bounds__(256) void ff_zero_kernel(ff_mat m, int64_t rows, in
     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) ff_store<FF_TANY, 4>(zero, m, i / cols, i % cols, 1);
 }
-
-// workgroups along the rows: enough to fill the chip, few enough for the column sums
-unsigned row_blocks(int64_t rows, unsigned strips) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, FFE_ROWS), std::max(1u, 2048 / strips))); }
 
 unsigned flat_blocks(int64_t n) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(cdiv(n, 256), 1 << 16)); }
 
@@ -264,7 +267,10 @@ int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pc
     if (Z1) { a.Z1 = *Z1; a.D1 = *D1; }
     const bool all16 = dY.b16 && Z0.b16 && (!Z1 || Z1->b16) && D0.b16, all32 = !dY.b16 && !Z0.b16 && (!Z1 || !Z1->b16) && !D0.b16;
     const int v = all32 ? 4 : 8, outs = Z1 ? 2 : 1;
-    const unsigned strips = cdiv(pcols, FFE_CH * v), blocks = row_blocks(rows, strips);
+    const int64_t chunks = cdiv(pcols, v);
+    const unsigned ch = chunks <= 8 ? 8 : (chunks <= 16 ? 16 : 32), strips = cdiv(chunks, ch);
+    // workgroups along the rows: enough to fill the chip, few enough for the column sums
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, 256 / ch), std::max(1u, 2048 / strips)));
     const bool sums = db[0] || (Z1 && db[1]);
     const size_t off = ws->off;
     if (sums) {
@@ -272,7 +278,13 @@ int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pc
         if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
     }
     const dim3 grid(strips, blocks), block(256);
-#define SGNN_FFE(T_, V_, G_) SGNN_LAUNCH(ctx, st, "ff_act_bwd_kernel", SGNN_TAG, (ff_act_bwd_kernel<T_, V_, G_>), grid, block, 0, st, a)
+#define SGNN_FFE_CH(T_, V_, G_, CH_) SGNN_LAUNCH(ctx, st, "ff_act_bwd_kernel", SGNN_TAG, (ff_act_bwd_kernel<T_, V_, G_, CH_>), grid, block, 0, st, a)
+#define SGNN_FFE(T_, V_, G_)                             \
+    do {                                                 \
+        if (ch == 8) SGNN_FFE_CH(T_, V_, G_, 8);         \
+        else if (ch == 16) SGNN_FFE_CH(T_, V_, G_, 16);  \
+        else SGNN_FFE_CH(T_, V_, G_, 32);                \
+    } while (0)
     if (Z1) {
         if (all16) SGNN_FFE(FF_T16, 8, true);
         else if (all32) SGNN_FFE(FF_T32, 4, true);
@@ -283,8 +295,9 @@ int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pc
         else SGNN_FFE(FF_TANY, 8, false);
     }
 #undef SGNN_FFE
+#undef SGNN_FFE_CH
     if (sums)
-        SGNN_LAUNCH(ctx, st, "ff_colsum_kernel", SGNN_TAG, ff_colsum_kernel, dim3(cdiv(outs * cols, 64)), dim3(1024), 0, st, a.partial, (int)blocks, (int)cols,
+        SGNN_LAUNCH(ctx, st, "ff_colsum_kernel", SGNN_TAG, ff_colsum_kernel, dim3(cdiv(outs * cols, 16)), dim3(1024), 0, st, a.partial, (int)blocks, (int)cols,
                     outs, db[0], Z1 ? db[1] : nullptr);
     ws->off = off;
     return SGNN_OK;
@@ -306,21 +319,33 @@ int sgnn_launch_ff_convert(sgnn_ctx *ctx, const ff_mat &src, int64_t rows, int64
     return SGNN_OK;
 }
 
-int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *word, hipStream_t st)
+// workgroups of a launch: one for every 256 / G rows up to as many as may leave a word each
+unsigned sgnn_ff_row_groups(int64_t rows, int64_t cols)
+{
+    const int64_t chunks = cdiv(cols, 8), per = chunks <= 16 ? 16 : (chunks <= 32 ? 8 : 4);
+    return (unsigned)std::min<int64_t>(std::max<int64_t>(cdiv(rows, per), 1), FF_ROW_WORDS);
+}
+
+unsigned sgnn_ff_scan_groups(int n, const ff_scan *w)
+{
+    int64_t most = 1;
+    for (int i = 0; i < n; ++i) most = std::max<int64_t>(most, w[i].rows * w[i].cols);
+    return (unsigned)std::min<int64_t>(cdiv(most, 256 * 8), FF_SCAN_WORDS);
+}
+
+int sgnn_launch_ff_row_parts(sgnn_ctx *ctx, const ff_row_parts &r, int n, const ff_scan *w, uint32_t *largest, hipStream_t st)
 {
     ffe_rows s = {};
     s.r = r;
-    s.word = word;
-    int64_t most = 0;
-    for (int i = 0; i < n; ++i) {
-        s.w[i] = w[i];
-        most = std::max(most, w[i].rows * w[i].cols);
-    }
+    s.largest = largest;
+    for (int i = 0; i < n; ++i) s.w[i] = w[i];
+    s.scans = n ? (int)sgnn_ff_scan_groups(n, w) : 0;
     const int64_t chunks = cdiv(r.m.cols, 8);
     auto run = [&](auto g, auto ch) -> int {
         constexpr int G = decltype(g)::value, CH = decltype(ch)::value;
-        const unsigned blocks = (unsigned)std::min<int64_t>(std::max<int64_t>(cdiv(r.m.rows, 256 / G), std::min<int64_t>(cdiv(most, 256 * 8), 512)), 4096);
-        SGNN_LAUNCH(ctx, st, "ff_row_parts_kernel", SGNN_TAG, (ff_row_parts_kernel<G, CH>), dim3(blocks, 1 + n), dim3(256), 0, st, s);
+        const unsigned rows = sgnn_ff_row_groups(r.m.rows, r.m.cols);
+        // the workgroups of y = 0 beyond those of the rows find none (and would leave words nobody counts)
+        SGNN_LAUNCH(ctx, st, "ff_row_parts_kernel", SGNN_TAG, (ff_row_parts_kernel<G, CH>), dim3(std::max(rows, (unsigned)s.scans), 1 + n), dim3(256), 0, st, s, rows);
         return SGNN_OK;
     };
     // the fewest lanes that hold a row, one chunk each up to a wavefront

@@ -46,7 +46,6 @@ struct ffg_args {
     int slices, per_split;            // slices of BK along the whole reduction, and of one range of it
     float *partial;                   // tn: [splits][mats][M][N]; else, where the reduction is split: [tiles][splits][BM BN]
     uint32_t *arrived;                // [tiles], zero between calls
-    uint32_t *clear;                  // two words that the next call wants at zero, or null
 };
 
 // Operand of R rows (or columns) by BK reduction steps in LDS.  PL = 2: the 16-byte chunks of the two parts alternate in a row.
@@ -84,7 +83,6 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
     const uint32_t per_mat = a.mtiles * a.ntiles, tiles = per_mat * a.mats * a.splits, run = (tiles + 7) / 8;
     const uint32_t id = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= run || id >= tiles) return;
-    if (a.clear && id == 0 && threadIdx.x < 2) a.clear[threadIdx.x] = 0;
     const uint32_t z = id / (per_mat * a.mats), t = id % (per_mat * a.mats), cols = a.ntiles * a.mats, group = t / (4 * cols);
     const uint32_t gm = min(4u, a.mtiles - 4 * group), in = t % (4 * cols);
     const uint32_t bm = 4 * group + in % gm, bc = in / gm, mat = bc / a.ntiles, bn = bc % a.ntiles;
@@ -255,13 +253,22 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
+                    // four ranges are requested together
                     f32x16 sum;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum[r] = 0.f;
-                    for (uint32_t y = 0; y < a.splits; ++y)
+                    for (uint32_t y0 = 0; y0 < a.splits; y0 += 4) {
+                        float v[4][16];
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            sum[r] += __hip_atomic_load(from + (size_t)y * (BM * BN) + ((i * TN + j) * 16 + r) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                v[u][r] = __hip_atomic_load(from + (size_t)min(y0 + u, a.splits - 1) * (BM * BN) + ((i * TN + j) * 16 + r) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) sum[r] += y0 + u < a.splits ? v[u][r] : 0.f;
+                    }
                     acc[i][j] = sum;
                 }
         }
@@ -333,24 +340,35 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
     }
 }
 
-// C[s] = sum over the ranges of partial[range][s], in their order
-__global__ __launch_bounds__(256) void ff_reduce_kernel(const float *__restrict__ partial, int splits, int mats, int64_t M, int N, ff_mat C0, ff_mat C1)
+// C[s] = sum over the ranges of partial[range][s]: ZL interleaved chains (the more, the fewer elements there are), then the chains in order
+template <int ZL> __global__ __launch_bounds__(256) void ff_reduce_kernel(const float *__restrict__ partial, int splits, int mats, int64_t M, int N, ff_mat C0, ff_mat C1)
 {
-    const int chunks = (N + 3) / 4;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = M * chunks;
-    if (i >= n * mats) return;
-    const int mat = (int)(i / n);
-    const int64_t row = (i % n) / chunks;
-    const int col = 4 * (int)(i % chunks), left = N - col;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    __shared__ f32x4 red[ZL > 1 ? 256 : 1];
+    const int chunks = (N + 3) / 4, zl = threadIdx.x / (256 / ZL);
+    const int64_t i = (int64_t)blockIdx.x * (256 / ZL) + threadIdx.x % (256 / ZL), n = M * chunks;
+    const bool in = i < n * mats;
+    const int mat = in ? (int)(i / n) : 0;
+    const int64_t row = in ? (i % n) / chunks : 0;
+    const int col = in ? 4 * (int)(i % chunks) : 0, left = N - col;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (in) {
 #pragma unroll 8
-    for (int z = 0; z < splits; ++z) {
-        float v[4];
-        ff_load<FF_T32, 4>(v, ff_mat{partial + ((int64_t)z * mats + mat) * M * N, N, 0}, row, col, left);
+        for (int z = zl; z < splits; z += ZL) {
+            float v[4];
+            ff_load<FF_T32, 4>(v, ff_mat{partial + ((int64_t)z * mats + mat) * M * N, N, 0}, row, col, left);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += v[e];
+            for (int e = 0; e < 4; ++e) s[e] += v[e];
+        }
     }
-    ff_store<FF_TANY, 4>(s, mat ? C1 : C0, row, col, left);
+    if constexpr (ZL > 1) {
+        red[threadIdx.x] = s;
+        __syncthreads();
+        if (zl) return;
+#pragma unroll
+        for (int q = 1; q < ZL; ++q) s += red[q * (256 / ZL) + threadIdx.x];
+    }
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    if (in) ff_store<FF_TANY, 4>(v, mat ? C1 : C0, row, col, left);
 }
 
 template <int PL, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, bool BTR, int KIND> int launch(sgnn_ctx *ctx, ffg_args a, int64_t splits, ws_alloc *ws, hipStream_t st)
@@ -370,7 +388,7 @@ template <int PL, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, 
         if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
     }
     if (joined) {
-        a.arrived = sgnn_ff_words(ctx).arrived;
+        a.arrived = sgnn_ff_arrived(ctx);
         const int rc = sgnn_ff_open(ctx, st);
         if (rc) return rc;
     }
@@ -389,18 +407,29 @@ template <int PL, int BM, int BN, int WM, int WN, int BK, int STAGES, bool ATR, 
     return rc;
 }
 
-// tile sizes, and ranges of the reduction
+// Tiles, by how many of them a compute unit has at a time (in LDS):
+//   WIDE   bfloat16 256 x 256, fp32 256 x 128, one;   TALL   bfloat16 256 x 128, two;   MID   128 x 128, two;   SMALL   64 x 128, two
 enum { FFT_WIDE, FFT_TALL, FFT_MID, FFT_SMALL };
 
-// Tiles of BM x BN for a result of M x N (both projections counted), K steps of the reduction.
+// Tile for a result of M x N (both projections counted) and K steps of the reduction, and the ranges that is split into.
+// The wide tile reads the least of LDS a product, but is alone on its compute unit: nothing runs while it fills its pipeline and writes its result.  bfloat16, us WIDE /
+// TALL / MID: 8192 x 8192 x 8192 920 / 1123 / 1196, 131072 x 256 x 1408 116 / 149 / 145, 65536 x 1024 x 512 99 / 101 / 115; 262144 x 256 x 256 78 / 74 / 80, gated
+// 131072 x 2 x 704 x 256 192 / 162 / 184.  fp32, WIDE / MID: 4096 x 4096 x 4096 375 / 401, 16384 x 1024 x 2048 194 / 197, 65536 x 1024 x 512 279 / 251,
+// gated 32768 x 2 x 704 x 256 108 / 94.  Where the last round of wide tiles leaves most compute units idle, smaller ones are better: 16384 x 512 x 512, 128 tiles, 27 / 22 / 19.
+// Fewer middle tiles than compute units: 2048 x 1024 x 2048 MID / SMALL bfloat16 27 / 23, fp32 54 / 42; with as many, 4096 x 1024 x 1024, 18.2 / 18.4, 34.6 / 35.2.
 int tile_for(int pl, int64_t M, int64_t N, int64_t K, int64_t *splits)
 {
     auto tiles = [&](int64_t bm, int64_t bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn); };
     *splits = 1;
-    if (pl == 1 ? tiles(256, 256) >= 192 : tiles(256, 128) >= 192) return pl == 1 && K <= 256 ? FFT_TALL : FFT_WIDE;
-    if (tiles(128, 128) >= 256) return FFT_MID;
+    const int64_t mid = tiles(128, 128);
+    if (pl == 1) {
+        // rounds of tiles, a round of wide ones as the unit
+        const int64_t wide = cdiv(tiles(256, 256), 256) * 6, middle = cdiv(mid, 512) * 4;
+        if (K >= 512 ? wide <= middle && tiles(256, 256) >= 128 : tiles(256, 256) >= 256) return K >= 512 ? FFT_WIDE : FFT_TALL;
+    } else if (K >= 2048 && tiles(256, 128) >= 256) return FFT_WIDE;
+    if (mid >= 256) return FFT_MID;
     const int64_t n = tiles(64, 128), slices = cdiv(K, pl == 1 ? 64 : 32);
-    if (n <= 256) *splits = std::max<int64_t>(1, std::min<int64_t>(512 / n, slices / 4));
+    if (n <= SGNN_FFN_COUNTS) *splits = std::max<int64_t>(1, std::min<int64_t>(512 / n, slices / 4));
     return FFT_SMALL;
 }
 
@@ -408,20 +437,22 @@ template <bool ATR, bool BTR, int KIND> int launch_tile(sgnn_ctx *ctx, int pl, c
 {
     if (pl == 1) {
         if (tile == FFT_WIDE) return launch<1, 256, 256, 2, 4, 64, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
-        if (tile == FFT_TALL) return launch<1, 256, 128, 2, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+        if constexpr (KIND != FFK_PARTIAL) {
+            if (tile == FFT_TALL) return launch<1, 256, 128, 2, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+        }
         if (tile == FFT_MID) return launch<1, 128, 128, 2, 2, 64, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
         return launch<1, 64, 128, 2, 2, 64, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
     }
-    if (tile == FFT_WIDE || tile == FFT_TALL) return launch<2, 256, 128, 4, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+    if constexpr (KIND != FFK_PARTIAL) {
+        if (tile == FFT_WIDE) return launch<2, 256, 128, 4, 2, 32, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
+    }
     if (tile == FFT_MID) return launch<2, 128, 128, 2, 2, 32, 2, ATR, BTR, KIND>(ctx, a, splits, ws, st);
     return launch<2, 64, 128, 2, 2, 32, 3, ATR, BTR, KIND>(ctx, a, splits, ws, st);
 }
 
-// An fp32 product also clears the largest magnitudes: the parts have been made of them, and nothing reads them before the next call.
-ffg_args args(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const int32_t *ex_rows, const int32_t *ex)
+ffg_args args(int64_t M, int64_t N, int64_t K, const int32_t *ex_rows, const int32_t *ex)
 {
     ffg_args a = {};
-    if (ex) a.clear = sgnn_ff_words(ctx).key;
     a.M = M; a.N = (int)N; a.K = K; a.segs = a.mats = 1;
     a.ex_rows = ex_rows; a.ex = ex;
     a.e.act = SGNN_ACT_NONE;
@@ -433,7 +464,7 @@ ffg_args args(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const int32_t *ex_
 int sgnn_launch_ff_nn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
                       const ff_epilogue &e, ws_alloc *ws, hipStream_t st)
 {
-    ffg_args a = args(ctx, M, N, K, ex_rows, ex);
+    ffg_args a = args(M, N, K, ex_rows, ex);
     a.A[0] = a.A[1] = A;
     a.B[0] = B[0];
     a.B[1] = B[mats - 1];
@@ -449,7 +480,7 @@ int sgnn_launch_ff_nn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
 int sgnn_launch_ff_nt(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int segs, const ff_op *A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
                       const ff_mat &Y, ws_alloc *ws, hipStream_t st)
 {
-    ffg_args a = args(ctx, M, N, K, ex_rows, ex);
+    ffg_args a = args(M, N, K, ex_rows, ex);
     a.segs = segs;
     for (int s = 0; s < segs; ++s) { a.A[s] = A[s]; a.B[s] = B[s]; }
     a.e.Y = Y;
@@ -472,7 +503,7 @@ size_t sgnn_ff_gemm_ws_bytes(uint64_t d_in, uint64_t d_out)
 int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
                       const ff_mat *C, ws_alloc *ws, hipStream_t st)
 {
-    ffg_args a = args(ctx, M, N, K, ex_rows, ex);
+    ffg_args a = args(M, N, K, ex_rows, ex);
     a.mats = mats;
     a.A[0] = a.A[1] = A;
     for (int s = 0; s < mats; ++s) a.B[s] = B[s];
@@ -480,13 +511,14 @@ int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
     a.e.Z[0] = C[mats - 1];
     const int bk = pl == 1 ? 64 : 32;
     const int64_t slices = cdiv(K, bk);
-    // the widest tile that leaves a range of eight slices and more to a workgroup a compute unit
+    // The wide tile for long reductions, us WIDE / MID: bfloat16 256 x 1408 x 131072 120 / 130, 1024 x 1024 x 8192 37 / 26; fp32 256 x 1408 x 32768 77 / 75 (not taken
+    // there).  Ranges: as many as fill the chip once.
     auto tiles = [&](int64_t bm, int64_t bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn) * mats; };
     auto ranges = [&](int64_t n, int64_t total) { return std::max<int64_t>(1, std::min<int64_t>(slices / 4, total / n)); };
     int tile = FFT_SMALL;
-    int64_t n = tiles(64, 128), splits = ranges(n, 512);
-    const int64_t nw = pl == 1 ? tiles(256, 256) : tiles(256, 128), nm = tiles(128, 128);
-    if (M > 128 && N > 64 && nw * (slices / 8) >= 192) tile = FFT_WIDE, splits = ranges(nw, 256);
+    int64_t splits = ranges(tiles(64, 128), 512);
+    const int64_t nw = tiles(256, 256), nm = tiles(128, 128);
+    if (pl == 1 && M > 128 && N > 128 && nw * slices >= 24 * 256) tile = FFT_WIDE, splits = ranges(nw, 256);
     else if (M > 64 && nm * (slices / 4) >= 192) tile = FFT_MID, splits = ranges(nm, 512);
     const size_t off = ws->off;
     const int rc = launch_tile<true, true, FFK_PARTIAL>(ctx, pl, a, tile, splits, ws, st);
@@ -494,7 +526,14 @@ int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
     ws->off = off;         // the partial results stay where they are until the next launch
     const int64_t per = cdiv(slices, splits);
     if (per >= slices) return SGNN_OK;
-    SGNN_LAUNCH(ctx, st, "ff_reduce_kernel", SGNN_TAG, ff_reduce_kernel, dim3(cdiv(M * ((N + 3) / 4) * mats, 256)), dim3(256), 0, st,
-                reinterpret_cast<const float *>(ws->base + off), (int)cdiv(slices, per), mats, M, (int)N, C[0], C[mats - 1]);
+    const int64_t items = M * ((N + 3) / 4) * mats;
+    const float *partial = reinterpret_cast<const float *>(ws->base + off);
+    const int ranges_ = (int)cdiv(slices, per);
+#define SGNN_FFG_REDUCE(ZL_) \
+    SGNN_LAUNCH(ctx, st, "ff_reduce_kernel", SGNN_TAG, ff_reduce_kernel<ZL_>, dim3(cdiv(items, 256 / ZL_)), dim3(256), 0, st, partial, ranges_, mats, M, (int)N, C[0], C[mats - 1])
+    if (ranges_ >= 32 && items < 256 * 256) SGNN_FFG_REDUCE(16);
+    else if (ranges_ >= 8) SGNN_FFG_REDUCE(4);
+    else SGNN_FFG_REDUCE(1);
+#undef SGNN_FFG_REDUCE
     return SGNN_OK;
 }

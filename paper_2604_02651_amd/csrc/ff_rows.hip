@@ -1,8 +1,8 @@
 // Products of a few rows (a trained block that answers for single vertices) with a weight matrix of any size: linear, gated and nt, as in ff_gemm.hip.
 //
 // A few rows read every weight once for two flop a row: what bounds them is how many weights are on their way at a time.  So the weights go from memory
-// straight into operand registers, no LDS and no barrier before the last sum: a wavefront takes pieces of KS reduction steps by CB columns, the sixteen
-// (eight, four, for 32 and 64 rows) wavefronts of a workgroup take the pieces of a column strip in turn, and their sums meet in LDS.  Where the
+// straight into operand registers, no LDS and no barrier before the last sum: a wavefront takes pieces of KS reduction steps by CB columns, the up to
+// sixteen wavefronts of a workgroup take the pieces of a column strip in turn, and their sums meet in LDS.  Where the
 // strips are fewer than the chip's compute units the reduction is split over several workgroups as well: each leaves its sums in scratch, and
 // the last one to arrive adds them up in the order of the ranges (bit-reproducible) and applies the epilogue.  No second launch.
 //   bfloat16: v_mfma_f32_16x16x32_bf16, fp32: v_mfma_f32_16x16x4_f32 (exact products).  KS = 32 / 16, a lane holds KL = 8 / 4 steps of a row of X and of
@@ -31,9 +31,12 @@ struct ffr_args {
     uint32_t *arrived;                // [strips], zero between calls
 };
 
-template <int KIND, bool NN, int V, int RT, int MATS> __global__ __launch_bounds__(1024 / RT) void ff_rows_kernel(ffr_args a)
+// wavefronts of a workgroup: as many as may leave their sums in LDS, at most sixteen
+template <int V, int RT, int MATS> constexpr int rows_waves() { return std::min(16, 128 * 1024 / (MATS * 16 * RT * 16 * V * 4)); }
+
+template <int KIND, bool NN, int V, int RT, int MATS> __global__ __launch_bounds__((64 * rows_waves<V, RT, MATS>())) void ff_rows_kernel(ffr_args a)
 {
-    constexpr int NW = 16 / RT, KS = KIND == FFR_F32 ? 16 : 32, KL = KS / 4, CB = 16 * V, ROWS = 16 * RT, ES = KIND == FFR_BF16 ? 2 : 4;
+    constexpr int NW = rows_waves<V, RT, MATS>(), KS = KIND == FFR_F32 ? 16 : 32, KL = KS / 4, CB = 16 * V, ROWS = 16 * RT, ES = KIND == FFR_BF16 ? 2 : 4;
     constexpr int WD = NN ? KL * V * ES / 4 : V * KL * ES / 4;             // registers of a piece's weights
     __shared__ float red[MATS][NW][ROWS][CB];
     __shared__ uint32_t last;
@@ -254,7 +257,7 @@ template <int KIND, bool NN, int V, int RT, int MATS> __global__ __launch_bounds
 
 template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, ffr_args a, ws_alloc *ws, hipStream_t st)
 {
-    constexpr int KS = KIND == FFR_F32 ? 16 : 32, CB = 16 * V, NW = 16 / RT, ROWS = 16 * RT;
+    constexpr int KS = KIND == FFR_F32 ? 16 : 32, CB = 16 * V, NW = rows_waves<V, RT, MATS>(), ROWS = 16 * RT;
     a.strips = cdiv(a.N, CB);
     a.steps = a.segs * (int)cdiv(a.K, KS);
     const unsigned groups = cdiv(a.M, ROWS);
@@ -266,7 +269,7 @@ template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, 
     const size_t off = ws->off;
     if (a.splits > 1) {
         a.partial = ws->get<float>((size_t)tiles * a.splits * MATS * ROWS * CB);
-        a.arrived = sgnn_ff_words(ctx).arrived;
+        a.arrived = sgnn_ff_arrived(ctx);
         if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
         const int rc = sgnn_ff_open(ctx, st);
         if (rc) return rc;
