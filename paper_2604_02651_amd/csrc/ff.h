@@ -116,7 +116,7 @@ size_t sgnn_ff_gemm_ws_bytes(uint64_t d_in, uint64_t d_out);
 // nn: weights [K x N] (two: gated); else nt over segs segments.  SGNN_ERR_UNSUPPORTED (nothing launched) for projections stored differently
 int sgnn_launch_ff_rows(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int segs, int mats, bool nn, bool b16, const ff_mat *X, const ff_mat *W, const ff_epilogue &e,
                         ws_alloc *ws, hipStream_t st);
-int64_t sgnn_ff_rows_max(int64_t N, int64_t K);
+bool sgnn_ff_rows_take(bool b16, int64_t M, int64_t N, int64_t K, int mats);
 size_t sgnn_ff_rows_ws_bytes();
 
 // ---- ff_elem.hip --------------------------------------------------------------------------------

@@ -106,7 +106,7 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
     e.act = act;
     e.R = view(R);
     e.Y = view(Y);
-    if (M <= sgnn_ff_rows_max(N, K)) {
+    if (sgnn_ff_rows_take(b16, M, N, K, n)) {
         const ff_mat xv = view(X), wv[2] = {view(W[0]), view(W[n - 1])};
         rc = sgnn_launch_ff_rows(ctx, M, N, K, 1, n, true, b16, &xv, wv, e, &ws, st);
         if (rc != SGNN_ERR_UNSUPPORTED) return rc;
@@ -174,7 +174,7 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
         if (is_dy && !any_db) return SGNN_OK;
         return sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, n == 2 ? &z1 : nullptr, is_dy ? ff_mat{nullptr, 0, b16} : d0, n == 2 ? &d1 : nullptr, db, &ws, st);
     };
-    const bool few = dX && M <= sgnn_ff_rows_max(K, n * N);
+    const bool few = dX && sgnn_ff_rows_take(b16, M, K, n * N, 1);
     // the gradient of a few rows
     auto few_rows = [&]() -> int {
         ff_epilogue e = {};

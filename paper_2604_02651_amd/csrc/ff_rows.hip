@@ -304,8 +304,14 @@ template <bool NN, int MATS> int launch_kind(sgnn_ctx *ctx, const ffr_args &a, b
 
 } // namespace
 
-// The tile kernels have the call from this many rows on
-int64_t sgnn_ff_rows_max(int64_t N, int64_t K) { return 64; }
+// Which calls these kernels have: the fewest rows always (each weight is read once), more of them while the products are few, since every 64 rows (32
+// gated) read the weights again.  us here / tile kernels, M x K x N, bfloat16: 2048 x 256 x 256 6.2 / 8.4, 512 x 1024 x 1024 9.4 / 16, 1024 x 1024 x 1024 17 / 21,
+// 2048 x 1024 x 1024 31 / 22, 512 x 512 x 2048 13 / 14, 1024 x 512 x 2048 23 / 19, 64 x 4096 x 4096 23 / 21; fp32 (whose tile kernels take parts that are made first):
+// 512 x 1024 x 1024 27 / 34, 1024 x 1024 x 1024 40 / 35, 64 x 4096 x 4096 46 / 62, 100 x 4096 x 4096 72 / 66; gated 512 x 1024 x 2 x 1024 15 / 20, 38 / 36.
+bool sgnn_ff_rows_take(bool b16, int64_t M, int64_t N, int64_t K, int mats)
+{
+    return M <= (b16 ? 32 : 64) || (M <= 2048 && (double)M * (double)N * (double)K * mats <= 8e8);
+}
 
 size_t sgnn_ff_rows_ws_bytes() { return (size_t)512 * 2 * 64 * 64 * 4 + 256; }
 
