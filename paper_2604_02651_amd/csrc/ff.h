@@ -144,6 +144,10 @@ int sgnn_launch_ff_parts(sgnn_ctx *ctx, int n, const ff_parts *m, hipStream_t st
 // the rounding) to db[0], db[1] where they are wanted
 int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pcols, int act, const ff_mat &dY, const ff_mat &Z0, const ff_mat *Z1,
                            const ff_mat &D0, const ff_mat *D1, float *const *db, ws_alloc *ws, hipStream_t st);
+// The same of fp32 matrices straight into the parts of [D0 | D1] (p.to, p.ld, and p.ex, p.other, p.key as above, a word of key for each of the groups)
+unsigned sgnn_ff_act_bwd_parts_groups(int64_t rows, int64_t pcols);
+int sgnn_launch_ff_act_bwd_parts(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pcols, int act, const ff_mat &dY, const ff_mat &Z0, const ff_mat *Z1,
+                                 const ff_row_parts &p, float *const *db, ws_alloc *ws, hipStream_t st);
 // zeros; rows of ld elements, cols of them written
 int sgnn_launch_ff_zero(sgnn_ctx *ctx, const ff_mat &m, int64_t rows, int64_t cols, hipStream_t st);
 size_t sgnn_ff_sums_ws_bytes(uint64_t cols);

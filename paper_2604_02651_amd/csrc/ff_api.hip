@@ -166,6 +166,7 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     // [D0 | D1] in one matrix, each padded with zeros to whole 16-byte chunks; without an activation dY itself, if the products can read it
     const bool is_dy = !need_z && (!b16 || (is16(dY) && ff_chunked(dY->ptr, N, dY->ld)));
     const int64_t np = is_dy ? N : ff_pad8(N), ldd = is_dy ? dY->ld : n * np;
+    // (fp32: not written where the gradients become parts at once, see below)
     void *D = is_dy ? dY->ptr : (b16 ? static_cast<void *>(ws.get<u16>((size_t)M * ldd)) : static_cast<void *>(ws.get<float>((size_t)M * ldd)));
     if (!ws.ok) return no_scratch(ctx, name);
     const ff_mat d0 = {D, ldd, b16}, d1 = {b16 ? static_cast<void *>(static_cast<u16 *>(D) + np) : static_cast<void *>(static_cast<float *>(D) + np), ldd, b16};
@@ -238,7 +239,9 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     }
     // fp32: the gradients' rows are scaled by themselves, the rows of X so that with the gradients' all products have one scale (ff_gemm.hip)
     const bool tiles_dx = dX && !few, split = any_dw || tiles_dx;
-    rc = gradients();
+    // the gradients as parts at once where nothing else reads them and a row fits the registers
+    const unsigned in_registers = split && !few && !is_dy ? sgnn_ff_act_bwd_parts_groups(M, np) : 0;
+    if (!in_registers) rc = gradients();
     if (!rc && few) rc = few_rows();
     if (rc || !split) return rc;
     ff_op d[2];
@@ -253,7 +256,7 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     if (any_dw) {
         x = parts_op(&ws, M, K);
         ex_x = ws.get<int32_t>((size_t)M);
-        job[jobs++] = ff_parts{scan(X), key, (int)sgnn_ff_row_groups(M, n * np), ex_d, ex + 1, const_cast<u16 *>(x.p), x.ld};
+        job[jobs++] = ff_parts{scan(X), key, (int)(in_registers ? in_registers : sgnn_ff_row_groups(M, n * np)), ex_d, ex + 1, const_cast<u16 *>(x.p), x.ld};
     }
     for (; tiles_dx && nw < n; ++nw) {
         w[nw] = parts_op(&ws, K, N);
@@ -262,9 +265,14 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     if (!ws.ok) return no_scratch(ctx, name);
     const int words = nw * (int)sgnn_ff_scan_groups(nw, scans);
     for (int q = 0; q < nw; ++q) job[jobs++] = ff_parts{scans[q], largest, words, nullptr, ex, const_cast<u16 *>(w[q].p), w[q].ld};
-    if (any_dw) rc = sgnn_launch_ff_row_parts(ctx, ff_row_parts{scan(X), nullptr, 0, ex_x, nullptr, nullptr}, 0, nullptr, nullptr, st);
     const ff_scan ds = {static_cast<const float *>(D), M, n * np, ldd};
-    if (!rc) rc = sgnn_launch_ff_row_parts(ctx, ff_row_parts{ds, const_cast<u16 *>(d[0].p), d[0].ld, ex_d, ex_x, any_dw ? key : nullptr}, nw, scans, largest, st);
+    const ff_row_parts xr = {scan(X), nullptr, 0, ex_x, nullptr, nullptr}, dr = {ds, const_cast<u16 *>(d[0].p), d[0].ld, ex_d, ex_x, any_dw ? key : nullptr};
+    // the largest weights ride along with the first launch over rows
+    if (any_dw) rc = sgnn_launch_ff_row_parts(ctx, xr, nw, scans, largest, st);
+    if (in_registers) {
+        if (!rc && !any_dw) rc = sgnn_launch_ff_row_parts(ctx, ff_row_parts{{nullptr, 0, 8, 8}, nullptr, 0, nullptr, nullptr, nullptr}, nw, scans, largest, st);
+        if (!rc) rc = sgnn_launch_ff_act_bwd_parts(ctx, M, N, np, act, view(dY), z0, n == 2 ? &z1 : nullptr, dr, db, &ws, st);
+    } else if (!rc) rc = sgnn_launch_ff_row_parts(ctx, dr, any_dw ? 0 : nw, scans, largest, st);
     if (!rc) rc = sgnn_launch_ff_parts(ctx, jobs, job, st);
     if (!rc && any_dw) rc = weights(2, x, d, nullptr, ex + 1);
     if (!rc && tiles_dx) rc = sgnn_launch_ff_nt(ctx, 2, M, K, N, n, d, w, ex_d, ex, view(dX), &ws, st);

@@ -223,6 +223,103 @@ template <int G, int CH> __global__ __launch_bounds__(256) void ff_row_parts_ker
     }
 }
 
+// act_bwd of fp32 matrices straight into parts: a row's gradients (of both projections) stay in the registers of its G lanes, CH chunks of eight columns a
+// lane, until their largest magnitude is known.  What it saves is a write and a read of D.
+template <bool GATED, int G, int CH> __global__ __launch_bounds__(256) void ff_act_bwd_parts_kernel(ffe_args a, ff_row_parts p)
+{
+    constexpr int RPW = 256 / G;
+    __shared__ float red[RPW > 1 ? 256 * CH * 8 : 1];
+    __shared__ uint32_t row_max[4];
+    const int l = threadIdx.x % G, grp = threadIdx.x / G;
+    float s0[CH][8], s1[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s0[c][i] = s1[c][i] = 0.f;
+    int key = 0;
+    for (int64_t row = (int64_t)blockIdx.x * RPW + grp; row < a.rows; row += (int64_t)gridDim.x * RPW) {
+        float d0[CH][8], d1[CH][8], u[CH][8];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = 8 * (c * G + l), left = a.cols - col;
+            // behind the last column every value is 0, and so are the gradients there
+            ff_load<FF_T32, 8>(d0[c], a.dY, row, col, left);
+            ff_load<FF_T32, 8>(d1[c], a.Z0, row, col, left);
+            if (GATED) ff_load<FF_T32, 8>(u[c], a.Z1, row, col, left);
+        }
+        uint32_t largest = 0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            ff_with_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const ff_act_pair f = ff_act_both<decltype(act)::value>(d1[c][i]);
+                    const float dy = d0[c][i];
+                    d0[c][i] = dy * (GATED ? u[c][i] * f.d : f.d);
+                    d1[c][i] = dy * f.f;
+                }
+            });
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s0[c][i] += d0[c][i];
+                largest = finite_max(largest, d0[c][i]);
+                if (GATED) {
+                    s1[c][i] += d1[c][i];
+                    largest = finite_max(largest, d1[c][i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, o, 64));
+        if constexpr (G > 64) {
+            // one row a workgroup: its wavefronts reach the barriers together
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) row_max[threadIdx.x >> 6] = largest;
+            __syncthreads();
+            largest = max(max(row_max[0], row_max[1]), max(row_max[2], row_max[3]));
+        }
+        const int ex = exponent_of(largest, FF_EX_ZERO);
+        if (l == 0) p.ex[row] = ex;
+        if (p.other) key = max(key, FF_EX_KEY - ex - p.other[row]);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = 8 * (c * G + l);
+            if (col >= a.pcols) continue;
+            store_parts(d0[c], ex, p.to + row * p.ld + 2 * col);
+            if (GATED) store_parts(d1[c], ex, p.to + row * p.ld + 2 * (a.pcols + col));
+        }
+    }
+    if (p.key) {
+        const uint32_t t = block_max((uint32_t)key);
+        if (threadIdx.x == 0) p.key[blockIdx.x] = t;
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int q = 0; q < (GATED ? 2 : 1); ++q) {
+        float *o = a.partial + ((int64_t)blockIdx.x * (GATED ? 2 : 1) + q) * a.cols;
+        if constexpr (RPW == 1) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (8 * (c * G + l) + i < a.cols) o[8 * (c * G + l) + i] = q ? s1[c][i] : s0[c][i];
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) red[grp * (G * CH * 8) + 8 * (c * G + l) + i] = q ? s1[c][i] : s0[c][i];
+            __syncthreads();
+            for (int j = threadIdx.x; j < a.cols; j += 256) {
+                float t = 0.f;
+#pragma unroll
+                for (int w = 0; w < RPW; ++w) t += red[w * (G * CH * 8) + j];
+                o[j] = t;
+            }
+        }
+    }
+}
+
 struct ffe_parts { ff_parts m[3]; };
 
 __global__ __launch_bounds__(256) void ff_parts_kernel(ffe_parts s)
@@ -254,8 +351,8 @@ unsigned flat_blocks(int64_t n) { return (unsigned)std::max<int64_t>(1, std::min
 
 size_t sgnn_ff_sums_ws_bytes(uint64_t cols)
 {
-    // one partial sum a column, projection and workgroup along the rows: 2048 workgroups in all, or one for every strip of 128 columns
-    return 2 * 4 * std::max<uint64_t>(2048 * 256, cols) + 4 * 4 * cols + 512;
+    // one partial sum a column, projection and workgroup along the rows: of these 2048 in all strips, or for every strip one; 2048 for rows of up to 4096
+    return 2 * 4 * std::max<uint64_t>(std::max<uint64_t>(2048 * 256, cols), 2048 * std::min<uint64_t>(cols, 4096)) + 512;
 }
 
 int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pcols, int act, const ff_mat &dY, const ff_mat &Z0, const ff_mat *Z1,
@@ -299,6 +396,47 @@ int sgnn_launch_ff_act_bwd(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pc
     if (sums)
         SGNN_LAUNCH(ctx, st, "ff_colsum_kernel", SGNN_TAG, ff_colsum_kernel, dim3(cdiv(outs * cols, 16)), dim3(1024), 0, st, a.partial, (int)blocks, (int)cols,
                     outs, db[0], Z1 ? db[1] : nullptr);
+    ws->off = off;
+    return SGNN_OK;
+}
+
+// workgroups along the rows of act_bwd_parts, each with a word of key and a partial sum a column: 0 where the rows are too wide for it
+unsigned sgnn_ff_act_bwd_parts_groups(int64_t rows, int64_t pcols)
+{
+    const int64_t chunks = pcols / 8, per = chunks <= 16 ? 16 : (chunks <= 32 ? 8 : (chunks <= 128 ? 4 : 1));
+    return chunks > 512 ? 0 : (unsigned)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, per), 2048));
+}
+
+int sgnn_launch_ff_act_bwd_parts(sgnn_ctx *ctx, int64_t rows, int64_t cols, int64_t pcols, int act, const ff_mat &dY, const ff_mat &Z0, const ff_mat *Z1,
+                                 const ff_row_parts &p, float *const *db, ws_alloc *ws, hipStream_t st)
+{
+    ffe_args a = {};
+    a.rows = rows; a.cols = (int)cols; a.pcols = (int)pcols; a.act = act;
+    a.dY = dY; a.Z0 = Z0;
+    if (Z1) a.Z1 = *Z1;
+    const int outs = Z1 ? 2 : 1;
+    const unsigned groups = sgnn_ff_act_bwd_parts_groups(rows, pcols);
+    const bool sums = db[0] || (Z1 && db[1]);
+    const size_t off = ws->off;
+    if (sums) {
+        a.partial = ws->get<float>((size_t)groups * outs * cols);
+        if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
+    }
+    auto run = [&](auto g, auto ch) -> int {
+        constexpr int G = decltype(g)::value, CH = decltype(ch)::value;
+        if (Z1) SGNN_LAUNCH(ctx, st, "ff_act_bwd_parts_kernel", SGNN_TAG, (ff_act_bwd_parts_kernel<true, G, CH>), dim3(groups), dim3(256), 0, st, a, p);
+        else SGNN_LAUNCH(ctx, st, "ff_act_bwd_parts_kernel", SGNN_TAG, (ff_act_bwd_parts_kernel<false, G, CH>), dim3(groups), dim3(256), 0, st, a, p);
+        return SGNN_OK;
+    };
+    const int64_t chunks = pcols / 8;
+    using std::integral_constant;
+    const int rc = chunks <= 16 ? run(integral_constant<int, 16>(), integral_constant<int, 1>()) : chunks <= 32 ? run(integral_constant<int, 32>(), integral_constant<int, 1>())
+                 : chunks <= 64 ? run(integral_constant<int, 64>(), integral_constant<int, 1>()) : chunks <= 128 ? run(integral_constant<int, 64>(), integral_constant<int, 2>())
+                 : chunks <= 256 ? run(integral_constant<int, 256>(), integral_constant<int, 1>()) : run(integral_constant<int, 256>(), integral_constant<int, 2>());
+    if (rc) return rc;
+    if (sums)
+        SGNN_LAUNCH(ctx, st, "ff_colsum_kernel", SGNN_TAG, ff_colsum_kernel, dim3(cdiv(outs * cols, 16)), dim3(1024), 0, st, a.partial, (int)groups, (int)cols, outs,
+                    db[0], Z1 ? db[1] : nullptr);
     ws->off = off;
     return SGNN_OK;
 }

@@ -1,0 +1,112 @@
+"""The feed-forward products at sizes that take every tile: many rows, long reductions, ragged edges.  The 64-bit formulas (ffn_ref.py, with its bounds) are
+evaluated for some rows of each result only."""
+import numpy as np
+import pytest
+import torch
+
+import ffn_ref as ref
+import paper_2604_02651_amd as sg
+from gpu_util import DEV
+from test_gpu_ffn import ACT, BF16, F32, TYPES, check, flags, operand_values, vec
+
+pytestmark = pytest.mark.gpu
+
+# M, K, N: more than 2048 rows, or many multiplications (others are the kernels' for few rows)
+SHAPES = [(2049, 33, 47), (2100, 2000, 100), (2500, 1000, 130), (2304, 1000, 1000), (4097, 100, 172), (1500, 1100, 600), (8200, 520, 1030), (16400, 64, 1030), (9000, 2056, 513),
+          (30011, 200, 531), (70, 4104, 3000)]
+_ctx = None
+
+
+def ctx():
+    global _ctx
+    if _ctx is None:
+        _ctx = sg.Context(0)
+        _ctx.reserve_ffn(50000, 1100, 1100)
+        _ctx.reserve_ffn(9000, 4200, 3000)
+    return _ctx
+
+
+def normal(shape, dtype, scale=1.0, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(shape, device=DEV, generator=g) * scale).to(dtype)
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def some(n, count=150):
+    """First, last and some in between"""
+    r = np.random.default_rng(n)
+    return np.unique(np.concatenate([[0, n - 1, n // 2], r.integers(0, n, min(n, count))]))
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_forward(shape, t):
+    M, K, N = shape
+    tx, tw, ty, tz = TYPES[t]
+    a = ref.ACTS[(M + len(t)) % 5]
+    print(shape, t, a, flush=True)
+    X, W, Wu, R = normal((M, K), tx, 1.0, 1), normal((K, N), tw, K ** -0.5, 2), normal((K, N), tw, K ** -0.5, 3), normal((M, N), ty, 1.0, 4)
+    X[M // 2] *= 2.0 ** -40 if t == "fp32" else 1.0           # a row of another magnitude
+    b = normal((N,), F32, 0.3, 5)
+    Y, Z, H, G, U = (torch.full((M, N), 77.0, dtype=d, device=DEV) for d in (ty, tz, ty, tz, tz))
+    rows = some(M)
+    x, w, wu, bb = operand_values(t, host(X[rows])), operand_values(t, host(W)), operand_values(t, host(Wu)), host(b)
+    sg.sgnn_linear_fwd(ctx(), X, W, b, ACT[a], flags(t), Y, R=R, Z=Z)
+    y, z = ref.linear_fwd(x, w, bb, a, host(R[rows]))
+    check(Z[rows], z, "Z"), check(Y[rows], y, "Y")
+    again = torch.empty_like(Y)
+    sg.sgnn_linear_fwd(ctx(), X, W, b, ACT[a], flags(t), again, R=R)
+    assert torch.equal(again, Y)
+    sg.sgnn_glu_fwd(ctx(), X, W, Wu, b, None, ACT[a], flags(t), H, G=G, U=U)
+    h, g, u = ref.glu_fwd(x, w, wu, bb, None, a)
+    check(G[rows], g, "G"), check(U[rows], u, "U"), check(H[rows], h, "H")
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("shape", SHAPES + [(50000, 512, 1030)], ids=str)
+def test_backward(shape, t):
+    M, K, N = shape
+    tx, tw, ty, tz = TYPES[t]
+    a = ref.ACTS[(M + len(t) + 1) % 5]
+    print(shape, t, a, flush=True)
+    X, W, Wu = normal((M, K), tx, 1.0, 1), normal((K, N), tw, K ** -0.5, 2), normal((K, N), tw, K ** -0.5, 3)
+    G, U, dY = normal((M, N), tz, 1.5, 4), normal((M, N), tz, 1.0, 5), normal((M, N), tx, 0.01, 6)
+    dY[M // 3] = 0
+    X[M // 3] = 3e30                   # a row that adds nothing, whatever its features hold
+    dX, dW, dWu = (torch.full(s, 77.0, dtype=ty, device=DEV) for s in ((M, K), (K, N), (K, N)))
+    db, du = (torch.full((N,), 77.0, device=DEV) for _ in range(2))
+    rows, cols = some(M, 60), some(K, 30)
+    w, wu, b16 = operand_values(t, host(W)), operand_values(t, host(Wu)), t != "fp32"
+    x = operand_values(t, host(X[:, cols]))
+
+    def verify(Ws, back, outs):
+        (dx, _, _) = back(rows)
+        check(dX[rows], dx, "dX")
+        (_, dws, dbs) = back(slice(None))
+        for i, (o, v) in enumerate(outs):
+            check(o[cols], dws[i], "dW%d" % i), check(v, dbs[i], "db%d" % i)
+
+    sg.sgnn_linear_bwd(ctx(), X, W, G, ACT[a], flags(t), dY, dX, dW, db)
+    g, u, d = host(G), host(U), host(dY)
+
+    def linear(r):
+        # all of the rows: a few columns of X are enough for the weights (and W's rows then do not matter)
+        return ref.linear_bwd(np.zeros((len(rows), 1)) if r is rows else x, w if r is rows else np.zeros((len(cols), N)), g[r], a, d[r], b16)
+    verify([w], linear, [(dW, db)])
+    again = torch.empty_like(dX)
+    sg.sgnn_linear_bwd(ctx(), X, W, G, ACT[a], flags(t), dY, again, None, None)
+    assert torch.equal(again, dX) or b16         # (bfloat16: both products together take another kernel than one)
+    check(again[rows], linear(rows)[0], "dX alone")
+    alone = torch.empty_like(dW)
+    sg.sgnn_linear_bwd(ctx(), X, W, G, ACT[a], flags(t), dY, None, alone, None)
+    check(alone[cols], linear(slice(None))[1][0], "dW alone")
+    if a == "none":
+        a = "silu"
+    sg.sgnn_glu_bwd(ctx(), X, W, Wu, G, U, ACT[a], flags(t), dY, dX, dW, dWu, dbg=db, dbu=du)
+
+    def gated(r):
+        return ref.glu_bwd(np.zeros((len(rows), 1)) if r is rows else x, *((w, wu) if r is rows else (np.zeros((len(cols), N)),) * 2), g[r], u[r], a, d[r], b16)
+    verify([w, wu], gated, [(dW, db), (dWu, du)])
