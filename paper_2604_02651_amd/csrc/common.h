@@ -153,10 +153,11 @@ int sgnn_launch_gemm_x(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, int6
                        const int32_t *a_row_index, const void *B, int b_bf16, int64_t ldb, const float *bias, int flags, void *C,
                        int c_bf16, int64_t ldc, const void *mask, int m_bf16, int64_t ldm, float *b_colsum, ws_alloc *ws,
                        hipStream_t st);
-// fp32 operands on the bfloat16 matrix pipe, split exactly (gemm_split.hip)
+// fp32 operands on the bfloat16 matrix pipe, split exactly (gemm_split.hip); e: the epilogue of a feed-forward operator, or null
+struct sgnn_split_epilogue { int used, act; const float *R; int64_t ldr; float *Z; int64_t ldz; };
 int sgnn_launch_gemm_split(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, int64_t K, const float *A, int64_t lda, const int32_t *ridx,
                            const float *B, int64_t ldb, const float *bias, int relu, float *C, int64_t ldc, const float *mask, int64_t ldm,
-                           float *b_colsum, ws_alloc *ws, hipStream_t st);
+                           float *b_colsum, ws_alloc *ws, hipStream_t st, const sgnn_split_epilogue *e = nullptr);
 // its form for a tall A and a small B (gemm_split_tall.hip)
 int sgnn_launch_gemm_split_tall(sgnn_ctx *ctx, int tb, int64_t M, int64_t N, int64_t K, const float *A, int64_t lda, const float *B, int64_t ldb,
                                 const float *bias, int relu, float *C, int64_t ldc, hipStream_t st);

@@ -28,8 +28,10 @@
 // (a softmax gradient has them where logits lie more than 65 apart): 32768 x 256 x 256 34 us, 122 if one tile or every
 // one holds one (fp32 instructions before: 47); 65536 x 256 x 608 134 us, 269 and 519 (189); 256 x 256 x 32768 42, 144 (48).
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
+#include "ff_act.h"
 
 namespace {
 
@@ -48,6 +50,7 @@ struct split_args {
     float *partial;               // [splits][M][N], or null
     float *colsum;                // column sums of B: [splits][N] when split
     uint32_t mtiles, ntiles, splits;
+    sgnn_split_epilogue e;        // of the feed-forward operators: C = act(Z) + R, Z = A B + bias, kept on request
 };
 
 constexpr int SBK = 32;                                     // slice of the reduction
@@ -373,18 +376,32 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_split_kernel(split_args 
             const int r = ((p0 + p) * NT + (int)threadIdx.x) / C4;
             if (m0 + r >= a.M) continue;
             f32x4 z = *reinterpret_cast<const f32x4 *>(tile + r * LDT + c0);
+            auto store = [&](float *o) {
+                if (whole) *reinterpret_cast<f32x4_any *>(o) = z;
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < a.N) o[e] = z[e];
+            };
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 z[e] += bj[e];
                 if (!plain && a.relu) z[e] = fmaxf(z[e], 0.f);
                 if (!plain && a.mask && !(m[p][e] > 0.f)) z[e] = 0.f;
             }
-            float *o = out + (m0 + r) * ldo + col;
-            if (whole) *reinterpret_cast<f32x4_any *>(o) = z;
-            else
+            if (a.e.used) {
+                if (a.e.Z) store(a.e.Z + (m0 + r) * a.e.ldz + col);
+                ff_with_act(a.e.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + e < a.N) o[e] = z[e];
+                    for (int e = 0; e < 4; ++e) z[e] = ff_act<decltype(act)::value>(z[e]);
+                });
+                if (a.e.R) {
+                    const float *rp = a.e.R + (m0 + r) * a.e.ldr;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] += rp[min(col + e, a.N - 1)];
+                }
+            }
+            store(out + (m0 + r) * ldo + col);
         }
     }
 }
@@ -424,9 +441,10 @@ int launch_split(sgnn_ctx *ctx, int ta, int tb, split_args a, hipStream_t st)
 // direction (the caller has checked).
 int sgnn_launch_gemm_split(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, int64_t K, const float *A, int64_t lda, const int32_t *ridx,
                            const float *B, int64_t ldb, const float *bias, int relu, float *C, int64_t ldc, const float *mask, int64_t ldm,
-                           float *b_colsum, ws_alloc *ws, hipStream_t st)
+                           float *b_colsum, ws_alloc *ws, hipStream_t st, const sgnn_split_epilogue *e)
 {
     split_args a = {};
+    if (e) a.e = *e;
     a.M = M; a.N = N; a.K = K; a.A = A; a.lda = lda; a.ridx = ridx; a.B = B; a.ldb = ldb; a.bias = bias; a.C = C; a.ldc = ldc;
     a.relu = relu; a.mask = mask; a.ldm = ldm; a.kps = K; a.splits = 1; a.colsum = b_colsum;
     // The widest tile of which there are enough for the 256 compute units: a 256 x 128 tile splits an element of A for 128
@@ -436,7 +454,7 @@ int sgnn_launch_gemm_split(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, 
     // Long reductions make up for few tiles with ranges, so A^T B takes the wide tile there as well, 256 x 256 x 32768 43 / 50, and
     // 128 x 64 from half that length on: 608 x 256 x 8000 50 us, 67 with 64 x 64, which is only better where it holds all
     // of M (40 x 256 x 50000 43 us, 52).
-    const bool plain = !bias && !relu && !mask;
+    const bool plain = !bias && !relu && !mask && !e;
     const bool long_ab = !ta && plain && K >= 4096;      // A B and A B^T too, where the tiles alone do not fill the chip
     const int64_t t256 = (int64_t)cdiv(M, 256) * cdiv(N, 128), t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128);
     int64_t bm = 64, bn = 64;
@@ -446,7 +464,7 @@ int sgnn_launch_gemm_split(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, 
     else if (!long_ab && ((int64_t)cdiv(M, 128) * cdiv(N, 64) >= 256 || (ta && M > 64 && K >= 4096))) bm = 128;
     // More tiles than compute units: the second round is a whole one however few they are, where the kernel for a tall A goes on slice by slice.  us
     // there / here, N = 256: 16384 x 256 22 / 25, 20000 x 256 37 / 28 (128 x 128 tiles up to there), 32768 x 256 32 / 33, 40000 x 256 59 / 43, 200000 x 128 127 / 91.
-    if (!ta && !ridx && !mask && bn == 128 && (bm == 256 ? t256 : t128) > 256) {
+    if (!ta && !ridx && !mask && !e && bn == 128 && (bm == 256 ? t256 : t128) > 256) {
         const int rc = sgnn_launch_gemm_split_tall(ctx, tb, M, N, K, A, lda, B, ldb, bias, relu, C, ldc, st);
         if (rc != SGNN_ERR_UNSUPPORTED) return rc;
     }
