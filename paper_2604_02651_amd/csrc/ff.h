@@ -107,6 +107,9 @@ int sgnn_launch_ff_nn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
 // Y = sum over s < segs of A[s] B[s]^T; A[s] [M x K], B[s] [N x K], laid out alike
 int sgnn_launch_ff_nt(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int segs, const ff_op *A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
                       const ff_mat &Y, ws_alloc *ws, hipStream_t st);
+// D[s], the gradients of the pre-activations Z (side by side in D [M x mats N], or D null), and dX [M x K] = sum over s of D[s] W[s]^T; or SGNN_ERR_UNSUPPORTED
+int sgnn_launch_ff_dx(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int mats, int act, const ff_mat &dY, const ff_mat *Z, const ff_op *W, const ff_mat &D, const ff_mat &dX,
+                      hipStream_t st);
 // C[s] = A^T B[s] for s < mats; A [K x M], B[s] [K x N], laid out alike
 int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
                       const ff_mat *C, ws_alloc *ws, hipStream_t st);

@@ -203,9 +203,32 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     };
     ff_op x, w[2];
     if (b16) {
-        rc = gradients();
-        if (rc) return rc;
+        // two projections laid out alike, by packing both if they are not
+        const bool pack = n == 2 && (W[0]->ld != W[1]->ld || is16(W[0]) != is16(W[1]) || ff_chunked(W[0]->ptr, N, W[0]->ld) != ff_chunked(W[1]->ptr, N, W[1]->ld));
+        auto weight_operands = [&]() -> int {
+            for (int q = 0; q < n; ++q) {
+                const int e = operand(ctx, name, W[q], pack, &ws, st, &w[q]);
+                if (e) return e;
+            }
+            return SGNN_OK;
+        };
         bool dx_done = false;
+        // D and dX in one pass (ff_dx.hip), where no sums over the rows of D are asked for.  A workgroup has 128 rows: it takes many of them, or few steps each.  Both
+        // operators' whole backward passes with it and without, us: gated, 256 columns of X, 704 of W, 131072 rows 348 and 438, 32768 96 and 125, 16384
+        // 68 and 72, 8192 60 and 56; 8192 x 256 x 128 26.7 and 27.1; linear 131072 x 256 x 512 186 and 214, 32768 x 256 x 256 41 and 61, 8192 x 256 x 256
+        // 31 and 50, 16384 x 128 x 1024 69 and 63.  A linear pass onto up to 128 columns of many rows has both products in one already (below):
+        // 131072 x 256 x 128 87 and 81, 49152 x 256 x 128 47 and 53.
+        if (dX && !few && !any_db && need_z && K <= 256 && (M >= 32768 || (M >= 8192 && K > 128 && N <= 512)) && !(n == 1 && N <= 128 && M >= 65536)) {
+            const size_t off = ws.off;
+            const ff_mat z[2] = {z0, z1};
+            rc = weight_operands();
+            if (!rc) rc = sgnn_launch_ff_dx(ctx, M, N, K, n, act, view(dY), z, w, any_dw ? d0 : ff_mat{nullptr, 0, 1}, view(dX), st);
+            if (rc != SGNN_OK && rc != SGNN_ERR_UNSUPPORTED) return rc;
+            dx_done = rc == SGNN_OK;
+            ws.off = off;
+        }
+        if (!dx_done) rc = gradients();
+        if (rc) return rc;
         if (few) {
             rc = few_rows();
             if (rc != SGNN_OK && rc != SGNN_ERR_UNSUPPORTED) return rc;
@@ -238,12 +261,8 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
             ws.off = off;
         }
         if (!dX || dx_done) return SGNN_OK;
-        // two projections laid out alike, by packing both if they are not
-        const bool pack = n == 2 && (W[0]->ld != W[1]->ld || is16(W[0]) != is16(W[1]) || ff_chunked(W[0]->ptr, N, W[0]->ld) != ff_chunked(W[1]->ptr, N, W[1]->ld));
-        for (int q = 0; q < n; ++q) {
-            rc = operand(ctx, name, W[q], pack, &ws, st, &w[q]);
-            if (rc) return rc;
-        }
+        rc = weight_operands();
+        if (rc) return rc;
         return sgnn_launch_ff_nt(ctx, 1, M, K, N, n, d, w, nullptr, nullptr, view(dX), &ws, st);
     }
     // fp32: the gradients' rows are scaled by themselves, the rows of X so that with the gradients' all products have one scale (ff_gemm.hip)

@@ -110,3 +110,46 @@ def test_backward(shape, t):
     def gated(r):
         return ref.glu_bwd(np.zeros((len(rows), 1)) if r is rows else x, *((w, wu) if r is rows else (np.zeros((len(cols), N)),) * 2), g[r], u[r], a, d[r], b16)
     verify([w, wu], gated, [(dW, db), (dWu, du)])
+
+
+def padded(m, pad):
+    """m with `pad` columns of NaN behind every row"""
+    wide = torch.full((m.shape[0], m.shape[1] + pad), float("nan"), dtype=m.dtype, device=DEV)
+    wide[:, :m.shape[1]] = m
+    return wide[:, :m.shape[1]]
+
+
+# up to 256 columns of X, no gradients of biases: D and dX in one pass, and on either side of the rule for it
+@pytest.mark.parametrize("a", ref.ACTS)
+@pytest.mark.parametrize("shape", [(32900, 200, 264), (33001, 65, 1032), (32769, 8, 8), (8200, 256, 72), (8319, 129, 520), (65600, 136, 128), (8191, 256, 64)], ids=str)
+def test_backward_without_biases(shape, a):
+    M, K, N = shape
+    print(shape, a, flush=True)
+    kept = F32 if a == "gelu" else BF16
+    X, W, Wu = normal((M, K), BF16, 1.0, 1), normal((K, N), kept, K ** -0.5, 2), normal((K, N), kept, K ** -0.5, 3)
+    G, U, dY = padded(normal((M, N), BF16, 1.5, 4), 8), padded(normal((M, N), BF16, 1.0, 5), 16), padded(normal((M, N), BF16, 0.01, 6), 24)
+    if kept is BF16:
+        W, Wu = padded(W, 8), padded(Wu, 8)
+    dX = padded(torch.full((M, K), 77.0, dtype=kept, device=DEV), 8)
+    dW, dWu = (torch.full((K, N), 77.0, dtype=kept, device=DEV) for _ in range(2))
+    rows, cols = some(M, 60), some(K, 20)
+    x, w, wu = host(X[:, cols]), operand_values("bf16", host(W)), operand_values("bf16", host(Wu))
+    g, u, d = host(G), host(U), host(dY)
+    few, all_rows = np.zeros((len(rows), 1)), np.zeros((len(cols), N))
+
+    sg.sgnn_glu_bwd(ctx(), X, W, Wu, G, U, ACT[a], flags("bf16"), dY, dX, dW, dWu)
+    check(dX[rows], ref.glu_bwd(few, w, wu, g[rows], u[rows], a, d[rows], True)[0], "dX")
+    dws = ref.glu_bwd(x, all_rows, all_rows, g, u, a, d, True)[1]
+    check(dW[cols], dws[0], "dWg"), check(dWu[cols], dws[1], "dWu")
+    assert torch.isnan(dX.as_strided((M, 8), (K + 8, 1), K)).all()
+    for out in ((dX, None, None), (dX, None, dWu)):
+        before = dX.clone()
+        dX.fill_(77.0)
+        sg.sgnn_glu_bwd(ctx(), X, W, Wu, G, U, ACT[a], flags("bf16"), dY, *out)
+        assert torch.equal(dX, before)
+    check(dWu[cols], dws[1], "dWu alone")
+
+    sg.sgnn_linear_bwd(ctx(), X, W, G, ACT[a], flags("bf16"), dY, dX, dW, None)
+    check(dX[rows], ref.linear_bwd(few, w, g[rows], a, d[rows], True)[0], "dX")
+    check(dW[cols], ref.linear_bwd(x, all_rows, g, a, d, True)[1][0], "dW")
+    assert torch.isnan(dX.as_strided((M, 8), (K + 8, 1), K)).all()
