@@ -9,9 +9,9 @@
 
 struct ff_act_pair { float f, d; };       // act(z) and act'(z)
 
-// 1 / (1 + exp(-x)) from the exponential of -|x|, which cannot overflow.  QUICK, for results that are rounded to bfloat16: the exponential as 2^(-x log2 e) with the
-// rounding of that product, a relative error of up to 2^-17 where the result is not 0, against the 2^-9 of the rounding; 4 instructions instead of 15
-// (the products' last pass of bfloat16 values was bound by them)
+// 1 / (1 + exp(-x)) from the exponential of -|x|, which cannot overflow.  QUICK, beside products of bfloat16
+// operands: the exponential as 2^(-x log2 e) with the rounding of that product, x s(x) and its slope to within 2^-22 of the larger of |x| and 1, against
+// the 2^-9 of the operands' rounding; 4 instructions instead of 15 (gated product of 65536 x 256 x 704 97 -> 92 us, its backward pass, ff_dx.hip, 260 -> 253)
 template <bool QUICK = false> __device__ __forceinline__ float ff_logistic(float x)
 {
     if constexpr (QUICK) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269502162933349609375f));

@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN * PL >= 32768 ? 2 : 1) void f
                 if (KIND == FFK_LINEAR && ep.R.p) ff_load<FF_TANY, 8>(u, ep.R, row, col, cols_left);
                 ff_with_act(ep.act, [&](auto act) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = ff_act<decltype(act)::value>(v[e]);
+                    for (int e = 0; e < 8; ++e) v[e] = ff_act<decltype(act)::value, PL == 1>(v[e]);
                 });
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = KIND == FFK_GLU ? v[e] * u[e] : (ep.R.p ? v[e] + u[e] : v[e]);
