@@ -360,13 +360,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_split_kernel(split_args 
 #pragma unroll
     for (int e = 0; e < 4; ++e) bj[e] = (!plain && a.bias) ? a.bias[min(col + e, a.N - 1)] : 0.f;
     const float *side = a.mask ? a.mask : a.e.R;             // never both
-    const int64_t lds = a.mask ? a.ldm : a.e.ldr;
+    const int64_t side_ld = a.mask ? a.ldm : a.e.ldr;
     for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
         f32x4 m[BATCH];
         if (!plain && side) {
 #pragma unroll
             for (int p = 0; p < BATCH; ++p) {
-                const float *mp = side + min(m0 + ((p0 + p) * NT + (int)threadIdx.x) / C4, a.M - 1) * lds;
+                const float *mp = side + min(m0 + ((p0 + p) * NT + (int)threadIdx.x) / C4, a.M - 1) * side_ld;
                 if (whole) m[p] = *reinterpret_cast<const f32x4_any *>(mp + col);
                 else
 #pragma unroll
