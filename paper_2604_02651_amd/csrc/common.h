@@ -162,7 +162,7 @@ int sgnn_launch_gemm_split(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, 
 int sgnn_launch_gemm_split_tall(sgnn_ctx *ctx, int tb, int64_t M, int64_t N, int64_t K, const float *A, int64_t lda, const float *B, int64_t ldb,
                                 const float *bias, int relu, float *C, int64_t ldc, hipStream_t st);
 int sgnn_launch_splitk_reduce(sgnn_ctx *ctx, const float *partial, int splits, int64_t M, int64_t N, float *C, int64_t ldc,
-                              const float *cs_partial, float *cs_out, hipStream_t st);
+                              const float *cs_partial, float *cs_out, hipStream_t st, unsigned short *C16 = nullptr);
 // gemm_rows.hip: tall bfloat16 A times a small B, result (and mask) bfloat16
 int sgnn_launch_gemm_rows(sgnn_ctx *ctx, int tb, int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const int32_t *row_index, const float *B,
                           int64_t ldb, const float *bias, int relu, void *C, int64_t ldc, const void *mask, int64_t ldm, hipStream_t st);
@@ -175,7 +175,8 @@ int sgnn_launch_gemm_tn_stream(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, c
 // C = X^T D (and the column sums of D) and G = D W^T, masked by X on request, in one pass over X and D (gemm_bwd.hip): SGNN_ERR_UNSUPPORTED (nothing
 // launched) outside its range.  g_pad: the columns of G between M and ldg may be written
 int sgnn_launch_gemm_bwd(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const void *X, int64_t ldx, const void *D, int64_t ldd, const float *W,
-                         int64_t ldw, void *G, int64_t ldg, bool g_pad, bool mask, float *C, float *d_colsum, ws_alloc *ws, hipStream_t st);
+                         int64_t ldw, void *G, int64_t ldg, bool g_pad, bool mask, float *C, float *d_colsum, ws_alloc *ws, hipStream_t st,
+                         const unsigned short *W16 = nullptr, unsigned short *C16 = nullptr, int64_t ldc = 0);
 int sgnn_launch_gemm_tail(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const float *A, int64_t lda, const float *W,
                           int64_t ldw, const float *gamma, float eps, const float *R, int64_t ldr, float q, uint64_t seed,
                           uint32_t layer, uint64_t step, float *Z, int64_t ldz, float *Y, int64_t ldy, float *inv_rms,

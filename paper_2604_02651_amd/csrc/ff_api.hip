@@ -235,18 +235,20 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
             dx_done = rc == SGNN_OK;
         }
         const ff_op d[2] = {{static_cast<const u16 *>(d0.p), ldd}, {static_cast<const u16 *>(d1.p), ldd}};
-        // both products of many rows onto up to 256 columns in one pass over X and D (gemm_bwd.hip), which reads fp32 weights and writes an fp32 gradient
+        // both products of many rows onto up to 256 columns in one pass over X and D (gemm_bwd.hip)
         if (n == 1 && dX && dW[0] && !dx_done && is16(X) && is16(dX)) {
             const size_t off = ws.off;
-            const bool w32 = !is16(W[0]), direct = !is16(dW[0]) && dW[0]->ld == N;
-            float *wf = w32 ? static_cast<float *>(W[0]->ptr) : (K <= 256 && N <= 256 ? ws.get<float>((size_t)K * N) : nullptr);
-            float *cf = direct ? static_cast<float *>(dW[0]->ptr) : (K <= 256 && N <= 256 ? ws.get<float>((size_t)K * N) : nullptr);
-            if (wf && cf && ws.ok) {
-                // the weights are widened first: whether the kernel takes the call is known when it has been launched
-                if (!w32 && M >= 8192 && K > 64) rc = sgnn_launch_ff_convert(ctx, view(W[0]), K, N, ff_mat{wf, N, 0}, st);
+            const u16 *w16 = is16(W[0]) && ff_chunked(W[0]->ptr, N, W[0]->ld) ? static_cast<const u16 *>(W[0]->ptr) : nullptr;
+            const bool widen = is16(W[0]) && !w16 && M >= 8192 && K > 64 && K <= 256 && N <= 256;      // the kernel reads fp32 or whole 16-byte chunks
+            float *wide = widen ? ws.get<float>((size_t)K * N) : nullptr;
+            if (widen && ws.ok) {
+                rc = sgnn_launch_ff_convert(ctx, view(W[0]), K, N, ff_mat{wide, N, 0}, st);
                 if (rc) return rc;
-                rc = sgnn_launch_gemm_bwd(ctx, K, N, M, X->ptr, X->ld, D, ldd, wf, w32 ? W[0]->ld : N, dX->ptr, dX->ld, false, false, cf, nullptr, &ws, st);
-                if (rc == SGNN_OK) return direct ? SGNN_OK : sgnn_launch_ff_convert(ctx, ff_mat{cf, N, 0}, K, N, view(dW[0]), st);
+            }
+            if (!is16(W[0]) || w16 || (widen && ws.ok)) {
+                rc = sgnn_launch_gemm_bwd(ctx, K, N, M, X->ptr, X->ld, D, ldd, widen ? wide : (w16 ? nullptr : static_cast<const float *>(W[0]->ptr)), widen ? N : W[0]->ld, dX->ptr, dX->ld,
+                                          false, false, is16(dW[0]) ? nullptr : static_cast<float *>(dW[0]->ptr), nullptr, &ws, st, w16,
+                                          is16(dW[0]) ? static_cast<u16 *>(dW[0]->ptr) : nullptr, dW[0]->ld);
                 if (rc != SGNN_ERR_UNSUPPORTED) return rc;
             }
             ws.off = off;

@@ -26,7 +26,7 @@ constexpr int BWD_WAVES = 8, BWD_LDS = 160 * 1024;
 struct bwd_args {
     const u16 *X; int64_t ldx;      // [K x M], ldx a multiple of 8
     const u16 *D; int64_t ldd;      // [K x N], ldd a multiple of 8
-    const float *W; int64_t ldw;    // [M x N]
+    const float *W; const u16 *W16; int64_t ldw;     // [M x N], fp32, or (W null) bfloat16
     int M, N;
     int64_t K;
     u16 *G; int64_t ldg;
@@ -113,8 +113,20 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void gemm_bwd_kernel(bwd_args a)
 
     // the wavefront's 32 rows of W, zero beyond M and N: lane (li, kh) has columns 16 st + 8 kh .. + 7 of row 32 mt + li.  Four steps at a time:
     // all requested together they would spill, one by one they cost a round trip to memory each (8192 x 128 x 256 60 us instead of 34)
-    const float *w_row = a.W + (int64_t)min(32 * mt + li, a.M - 1) * a.ldw;
+    const int64_t w_off = (int64_t)min(32 * mt + li, a.M - 1) * a.ldw;
+    const float *w_row = a.W + w_off;
     auto w_pieces = [&](int st0, bf16x8 (&v)[4]) {
+        if (!a.W) {                              // N a multiple of eight
+            u32x4 x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = *reinterpret_cast<const u32x4 *>(a.W16 + w_off + min(16 * (st0 + q) + 8 * kh, a.N - 8));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                x[q] &= 32 * mt + li < a.M && 16 * (st0 + q) + 8 * kh < a.N ? 0xffffffffu : 0u;
+                v[q] = __builtin_bit_cast(bf16x8, x[q]);
+            }
+            return;
+        }
         float x[4][8];
         if (st0 + 4 < STEPS || WHOLE) {          // (a frame is at most 63 columns wider than N)
 #pragma unroll
@@ -373,8 +385,9 @@ inline bool overlap(const void *p, size_t n, const void *q, size_t m)
 
 // Returns SGNN_ERR_UNSUPPORTED without launching anything for what the kernel does not handle: the two products then run one after the
 // other.  g_pad: the columns of G between M and the leading dimension may be written.
+// W fp32, or W16 in its place (bfloat16, 16-byte chunks, N a multiple of eight).  C fp32, or C16 in its place (bfloat16); ldc 0: without padding.
 int sgnn_launch_gemm_bwd(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const void *X, int64_t ldx, const void *D, int64_t ldd, const float *W,
-                         int64_t ldw, void *G, int64_t ldg, bool g_pad, bool mask, float *C, float *d_colsum, ws_alloc *ws, hipStream_t st)
+                         int64_t ldw, void *G, int64_t ldg, bool g_pad, bool mask, float *C, float *d_colsum, ws_alloc *ws, hipStream_t st, const u16 *W16, u16 *C16, int64_t ldc)
 {
     constexpr int64_t LD_MAX = 1 << 20;          // offsets within a slice in 32 bits
     auto al16 = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
@@ -386,7 +399,7 @@ int sgnn_launch_gemm_bwd(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const v
     // operand would be written while others still read it
     const size_t gb = (size_t)K * ldg * 2;
     if ((overlap(G, gb, X, (size_t)K * ldx * 2) && !(G == X && ldg == ldx)) || overlap(G, gb, D, (size_t)K * ldd * 2) ||
-        overlap(G, gb, W, (size_t)M * ldw * 4))
+        (W16 ? overlap(G, gb, W16, (size_t)M * ldw * 2) : overlap(G, gb, W, (size_t)M * ldw * 4)))
         return SGNN_ERR_UNSUPPORTED;
     const int fa = M > 128 ? 256 : 128, fb = N > 192 ? 256 : (N > 128 ? 192 : (N > 64 ? 128 : 64)), bk = fa == 256 ? 32 : 64;
     // Narrow X and wide D: 64 columns of G for eight wavefronts at a time are little work beside the D that each of them reads, and with few rows the
@@ -403,7 +416,7 @@ int sgnn_launch_gemm_bwd(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const v
     const size_t need = (((size_t)groups * M * N * 4 + 255) & ~size_t(255)) + (((size_t)groups * N * 4 + 255) & ~size_t(255));
     if (!ws->base || ws->off + need > ws->cap) return SGNN_ERR_UNSUPPORTED;
     bwd_args a;
-    a.X = static_cast<const u16 *>(X); a.ldx = ldx; a.D = static_cast<const u16 *>(D); a.ldd = ldd; a.W = W; a.ldw = ldw;
+    a.X = static_cast<const u16 *>(X); a.ldx = ldx; a.D = static_cast<const u16 *>(D); a.ldd = ldd; a.W = W16 ? nullptr : W; a.W16 = W16; a.ldw = ldw;
     a.M = (int)M; a.N = (int)N; a.K = K;
     a.G = static_cast<u16 *>(G); a.ldg = ldg; a.g_cols = (int)g_cols; a.mask = mask;
     a.partial = ws->get<float>((size_t)groups * M * N);
@@ -419,5 +432,5 @@ int sgnn_launch_gemm_bwd(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, const v
     else if (fb == 128) rc = launch_bwd<128, 128, 64, 2, 4, 8>(ctx, a, grid, st);
     else rc = launch_bwd<128, 64, 64, 4, 2, 4>(ctx, a, grid, st);
     if (rc) return rc;
-    return sgnn_launch_splitk_reduce(ctx, a.partial, (int)groups, M, N, C, N, a.cs_partial, d_colsum, st);
+    return sgnn_launch_splitk_reduce(ctx, a.partial, (int)groups, M, N, C, ldc ? ldc : N, a.cs_partial, d_colsum, st, C16);
 }

@@ -12,6 +12,13 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));      //
 
 constexpr int RED_WAVES = 8, RED_U = 8;
 
+// the result in its type, bfloat16 rounded to nearest even
+__device__ __forceinline__ void put(float *C, unsigned short *C16, int64_t i, float v)
+{
+    if (C16) C16[i] = __builtin_bit_cast(unsigned short, (__bf16)v);
+    else C[i] = v;
+}
+
 // sum over z of src[z * n + i .. i + 3] for the block's 256 elements from i0 on, one element a thread of the first 256
 __device__ __forceinline__ float sum_partials(const float *__restrict__ src, int splits, int64_t n, int64_t i0, float (&lds)[RED_WAVES][256])
 {
@@ -52,7 +59,7 @@ __device__ __forceinline__ float sum_partials(const float *__restrict__ src, int
 }
 
 __global__ __launch_bounds__(64 * RED_WAVES) void splitk_reduce_kernel(const float *__restrict__ partial, int splits, int64_t MN, int64_t N,
-                                                                       float *__restrict__ C, int64_t ldc, const float *__restrict__ cs_partial,
+                                                                       float *__restrict__ C, unsigned short *__restrict__ C16, int64_t ldc, const float *__restrict__ cs_partial,
                                                                        float *__restrict__ cs_out, unsigned blocks)
 {
     __shared__ float lds[RED_WAVES][256];
@@ -64,12 +71,12 @@ __global__ __launch_bounds__(64 * RED_WAVES) void splitk_reduce_kernel(const flo
     }
     const int64_t i0 = (int64_t)blockIdx.x * 256, i = i0 + threadIdx.x;
     const float t = sum_partials(partial, splits, MN, i0, lds);
-    if (threadIdx.x < 256 && i < MN) C[(i / N) * ldc + (i % N)] = t;
+    if (threadIdx.x < 256 && i < MN) put(C, C16, (i / N) * ldc + (i % N), t);
 }
 
 // The same for few partial products, an element a thread and eight loads in flight: no sums to meet in LDS.
 __global__ __launch_bounds__(256) void splitk_reduce_few_kernel(const float *__restrict__ partial, int splits, int64_t MN, int64_t N,
-                                                                float *__restrict__ C, int64_t ldc, const float *__restrict__ cs_partial,
+                                                                float *__restrict__ C, unsigned short *__restrict__ C16, int64_t ldc, const float *__restrict__ cs_partial,
                                                                 float *__restrict__ cs_out)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -87,25 +94,25 @@ __global__ __launch_bounds__(256) void splitk_reduce_few_kernel(const float *__r
     }
     const float t = (s[0] + s[1]) + (s[2] + s[3]);
     if (cs) cs_out[i - MN] = t;
-    else C[(i / N) * ldc + (i % N)] = t;
+    else put(C, C16, (i / N) * ldc + (i % N), t);
 }
 
 } // namespace
 
-// C = sum of `splits` partial products [splits][M][N]; cs_out = the same for [splits][N] column sums (cs_partial may be null).
+// C, or in its place C16 in bfloat16, = sum of `splits` partial products [splits][M][N]; cs_out = the same for [splits][N] column sums (cs_partial may be null).
 int sgnn_launch_splitk_reduce(sgnn_ctx *ctx, const float *partial, int splits, int64_t M, int64_t N, float *C, int64_t ldc,
-                              const float *cs_partial, float *cs_out, hipStream_t st)
+                              const float *cs_partial, float *cs_out, hipStream_t st, unsigned short *C16)
 {
     // us of the whole A^T B with bfloat16 operands, eight wavefronts / an element a thread: 16 partial products of 608 x 256 23.3 / 22.4, of 256 x 256
     // 20.1 / 19.4, of 200 x 200 19.0 / 18.7, 24 of 300 x 300 22.5 / 22.0, of 256 x 172 19.6 / 19.9; fp32, 32 of 256 x 256 20.0 / 19.8, of 200 x 200
     // 18.8 / 19.3, 38 of 256 x 172 20.2 / 21.1, 64 of 256 x 256 27.3 / 28.1.
     if (splits <= 16 || (splits <= 32 && M * N >= 65536)) {
         SGNN_LAUNCH(ctx, st, "splitk_reduce_kernel", "few", splitk_reduce_few_kernel, dim3(cdiv(M * N + (cs_partial ? N : 0), 256)), dim3(256), 0, st,
-                    partial, splits, M * N, N, C, ldc, cs_partial, cs_out);
+                    partial, splits, M * N, N, C, C16, ldc, cs_partial, cs_out);
         return SGNN_OK;
     }
     const unsigned blocks = cdiv(M * N, 256), cs_blocks = cs_partial ? cdiv(N, 256) : 0;
     SGNN_LAUNCH(ctx, st, "splitk_reduce_kernel", SGNN_TAG, splitk_reduce_kernel, dim3(blocks + cs_blocks), dim3(64 * RED_WAVES), 0, st, partial,
-                splits, M * N, N, C, ldc, cs_partial, cs_out, blocks);
+                splits, M * N, N, C, C16, ldc, cs_partial, cs_out, blocks);
     return SGNN_OK;
 }

@@ -153,3 +153,20 @@ def test_backward_without_biases(shape, a):
     check(dX[rows], ref.linear_bwd(few, w, g[rows], a, d[rows], True)[0], "dX")
     check(dW[cols], ref.linear_bwd(x, all_rows, g, a, d, True)[1][0], "dW")
     assert torch.isnan(dX.as_strided((M, 8), (K + 8, 1), K)).all()
+
+
+# many rows onto up to 256 columns with the gradient of the bias: both products in one pass, weights and their gradient in either type
+@pytest.mark.parametrize("kept", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(8300, 96, 200), (9001, 256, 256), (8193, 72, 24), (12000, 200, 100), (8192, 248, 8)], ids=str)
+def test_backward_few_columns(shape, kept):
+    M, K, N = shape
+    print(shape, kept, flush=True)
+    X, W, Z, dY = normal((M, K), BF16, 1.0, 1), padded(normal((K, N), kept, K ** -0.5, 2), 8), normal((M, N), BF16, 1.5, 3), normal((M, N), BF16, 0.01, 4)
+    dX, dW, db = torch.full((M, K), 77.0, dtype=BF16, device=DEV), padded(torch.full((K, N), 77.0, dtype=kept, device=DEV), 5), torch.full((N,), 77.0, device=DEV)
+    rows, cols = some(M, 60), some(K, 20)
+    sg.sgnn_linear_bwd(ctx(), X, W, Z, ACT["silu"], flags("bf16"), dY, dX, dW, db)
+    z, d, w = host(Z), host(dY), operand_values("bf16", host(W))
+    check(dX[rows], ref.linear_bwd(np.zeros((len(rows), 1)), w, z[rows], "silu", d[rows], True)[0], "dX")
+    (_, dw, dbs) = ref.linear_bwd(host(X[:, cols]), np.zeros((len(cols), N)), z, "silu", d, True)
+    check(dW[cols], dw[0], "dW"), check(db, dbs[0], "db")
+    assert torch.isnan(dW.as_strided((K, 5), (N + 5, 1), N)).all()
