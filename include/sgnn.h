@@ -420,7 +420,8 @@ int sgnn_adam_step(sgnn_ctx *ctx, float *w, const float *g, float *m, float *v, 
 /*
  * Feed-forward block of a layer: products with activation and residual, a gated projection, and the norms around a block.
  *
- * Matrices are SGNN_F32, with products in fp32 precision, or with SGNN_BF16_MFMA (the only flag) each SGNN_F32 or SGNN_BF16 as the caller
+ * Matrices are SGNN_F32, with products in fp32 precision (each to 2^-21 of itself; in larger calls values below 2^-29 of the largest of their row of X or of
+ * the gradients, or of their weight matrix, may be off by 2^-51 of that largest), or with SGNN_BF16_MFMA (the only flag) each SGNN_F32 or SGNN_BF16 as the caller
  * likes: product operands are rounded to bfloat16 (nearest even), sums, activations and statistics are fp32, a result is rounded once as it is
  * stored.  SGNN_BF16 anywhere without the flag is SGNN_ERR_UNSUPPORTED.  Vectors (biases, scales, their gradients) are fp32.  Any width from
  * 1 to 2^24, any leading dimension and alignment; bfloat16 operands whose columns and leading dimension are multiples of 8 and that start on 16

@@ -2,7 +2,8 @@
 
 Bounds are per element.  H = 2^-8 (bfloat16) is the largest relative error of one rounding, E = 2^-24 that of an fp32 operation.  A sum of K products is off
 by at most (K + 4) E times the sum of their magnitudes, in whichever order it is added up (4: what the split of fp32 operands into three bfloat16
-parts leaves out, under 2 E, and its parts' own sums).  An activation of one argument is evaluated to within A = 2^-20 of max(|z|, 1): some ten fp32
+parts leaves out, under 2 E, and its parts' own sums; two fp16 parts leave out up to 8 E of a product, in kernels that sum in the pipe's blocks of 16 products, one
+rounding each: (K / 16 + 8) E, which is less from K = 5 on).  An activation of one argument is evaluated to within A = 2^-20 of max(|z|, 1): some ten fp32
 operations, each E, and a hardware exponential and reciprocal, an ulp each, with arguments up to 20 and more where the result is not 0.
 """
 import numpy as np
