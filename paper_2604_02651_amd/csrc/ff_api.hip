@@ -16,6 +16,18 @@ bool same(const sgnn_mat *a, const sgnn_mat *b) { return a && b && a->ptr && a->
 // one matrix as an input and the output that replaces it: laid out alike, or not the same at all
 bool other_layout(const sgnn_mat *a, const sgnn_mat *b) { return same(a, b) && (a->ld != b->ld || a->dtype != b->dtype); }
 
+// an output that is the same matrix as an input, or as another output
+bool clash(std::initializer_list<const sgnn_mat *> outs, std::initializer_list<const sgnn_mat *> ins)
+{
+    for (auto o = outs.begin(); o != outs.end(); ++o) {
+        for (const sgnn_mat *i : ins)
+            if (same(*o, i)) return true;
+        for (auto p = o + 1; p != outs.end(); ++p)
+            if (same(*o, *p)) return true;
+    }
+    return false;
+}
+
 constexpr int64_t FF_MAX_WIDTH = 1 << 24;
 
 int act_ok(sgnn_ctx *ctx, const char *name, int act, int flags)
@@ -89,8 +101,7 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
     }
     if (!ok) return sgnn_fail(ctx, SGNN_ERR_INVALID_ARG, "%s: null pointer, shape mismatch or leading dimension too small", name);
     if (any16 && !(flags & SGNN_BF16_MFMA)) return sgnn_fail(ctx, SGNN_ERR_UNSUPPORTED, "%s: bfloat16 storage goes with SGNN_BF16_MFMA only", name);
-    if (same(X, Y) || same(X, Z[0]) || same(Y, Z[0]) || same(R, Z[0]) || (n == 2 && (same(X, Z[1]) || same(Y, Z[1]) || same(Z[0], Z[1]))) ||
-        other_layout(R, Y))
+    if (clash({Y, Z[0], n == 2 ? Z[1] : nullptr}, {X, W[0], n == 2 ? W[1] : nullptr}) || same(R, Z[0]) || other_layout(R, Y))
         return sgnn_fail(ctx, SGNN_ERR_INVALID_ARG, "%s: an output is the same matrix as another argument", name);
     if (M == 0) return SGNN_OK;
     rc = bind(ctx);
@@ -120,7 +131,7 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
     }
     // fp32.  A product of at most 256 tiles of 256 x 128, one a compute unit, with a short K, or of many rows onto few columns: three parts split as X is
     // read and six products (gemm_split.hip) cost less than two parts of X made first, 8 bytes a value at the rate of a copy and two launches, and three
-    // products.  With Z and R, parts first against split as read: 32768 x 256 x 256 50 and 45.7 us, 131072 x 512 x 128 204 and 147, 8192 x 256 x 512 38
+    // products.  With Z and R, parts first against split as read: 32768 x 256 x 256 50 and 44 us, 131072 x 512 x 128 204 and 147, 8192 x 256 x 512 38
     // and 27; past the rule 131072 x 256 x 256 171 and 196, 32768 x 256 x 512 67 and 86, 4096 x 2048 x 256 48 and 71
     if (n == 1 && K >= 4 && N >= 4 && ((K <= 512 && ((M + 255) / 256) * ((N + 127) / 128) <= 256) || (N <= 128 && M >= 16384))) {
         const sgnn_split_epilogue se = {1, act, R ? static_cast<const float *>(R->ptr) : nullptr, R ? R->ld : 0, Z[0] ? static_cast<float *>(Z[0]->ptr) : nullptr, Z[0] ? Z[0]->ld : 0};
@@ -163,7 +174,8 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
     }
     if (!ok) return sgnn_fail(ctx, SGNN_ERR_INVALID_ARG, "%s: null pointer, shape mismatch or leading dimension too small", name);
     if (any16 && !b16) return sgnn_fail(ctx, SGNN_ERR_UNSUPPORTED, "%s: bfloat16 storage goes with SGNN_BF16_MFMA only", name);
-    if (same(dX, X) || same(dX, dY) || same(dX, Z[0]) || (n == 2 && (same(dX, Z[1]) || same(dW[0], dW[1]))))
+    const bool two = n == 2;
+    if (clash({dX, dW[0], two ? dW[1] : nullptr}, {X, dY, Z[0], W[0], two ? Z[1] : nullptr, two ? W[1] : nullptr}))
         return sgnn_fail(ctx, SGNN_ERR_INVALID_ARG, "%s: an output is the same matrix as another argument", name);
     const bool any_dw = dW[0] || (n == 2 && dW[1]), any_db = db[0] || (n == 2 && db[1]);
     if (!dX && !any_dw && !any_db) return SGNN_OK;

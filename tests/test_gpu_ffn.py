@@ -468,3 +468,25 @@ def test_refusals():
     small = sg.Context(0)
     refused(-2, sg.sgnn_linear_bwd, small, X, W, Y, 1, 0, Y, X.clone(), D, None)                # nothing reserved
     small.close()
+
+
+def test_outputs_over_inputs_are_refused():
+    c = ctx()
+    q = lambda: torch.zeros((16, 16), device=DEV)      # noqa: E731
+    X, W, V, Z, G, dY, Y, D = (q() for _ in range(8))
+
+    def refused(f, *a, **k):
+        with pytest.raises(sg.SgnnError) as e:
+            f(*a, **k)
+        assert e.value.code == -1, e.value
+    for y, z in ((W, None), (X, None), (Y, W), (Y, X), (Y, Y)):
+        refused(sg.sgnn_linear_fwd, c, X, W, None, 1, 0, y, Z=z)
+    refused(sg.sgnn_linear_fwd, c, X, W, None, 1, 0, Y, R=Z, Z=Z)
+    for h, g, u in ((V, None, None), (Y, V, None), (Y, None, W), (Y, Z, Z)):
+        refused(sg.sgnn_glu_fwd, c, X, W, V, None, None, 4, 0, h, G=g, U=u)
+    for dx, dw in ((W, None), (Z, None), (dY, None), (D, D), (None, W), (None, X), (None, dY), (None, Z)):
+        refused(sg.sgnn_linear_bwd, c, X, W, Z, 1, 0, dY, dx, dw, None)
+    for dx, dw, dv in ((V, None, None), (G, None, None), (None, V, None), (None, None, W), (None, D, D), (D, None, D)):
+        refused(sg.sgnn_glu_bwd, c, X, W, V, Z, G, 4, 0, dY, dx, dw, dv)
+    sg.sgnn_linear_fwd(c, X, X, None, 1, 0, Y, R=X)          # one matrix for several inputs is fine
+    sg.sgnn_linear_bwd(c, X, X, X, 1, 0, X, D, Y, None)

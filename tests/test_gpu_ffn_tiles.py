@@ -170,3 +170,91 @@ def test_backward_few_columns(shape, kept):
     (_, dw, dbs) = ref.linear_bwd(host(X[:, cols]), np.zeros((len(cols), N)), z, "silu", d, True)
     check(dW[cols], dw[0], "dW"), check(db, dbs[0], "db")
     assert torch.isnan(dW.as_strided((K, 5), (N + 5, 1), N)).all()
+
+
+# many rows and the narrowest matrices.  fp32: two fp16 parts leave out up to 8 E of a product, more than the bound of so few of them allows for
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(5000, 1, 5), (4099, 3, 1), (3000, 5, 3), (2050, 2, 130), (3001, 4, 4), (70000, 7, 2)], ids=str)
+def test_narrow(shape, t):
+    M, K, N = shape
+    print(shape, t, flush=True)
+    dt = TYPES[t][0]
+    X, W, Wu, R = normal((M, K), dt, 1.0, 1), normal((K, N), dt, 1.0, 2), normal((K, N), dt, 1.0, 3), normal((M, N), dt, 1.0, 4)
+    b, Y, Z, H = normal((N,), F32, 0.3, 5), *(torch.full((M, N), 77.0, dtype=dt, device=DEV) for _ in range(3))
+    x, w, wu, bb, r = host(X), host(W), host(Wu), host(b), host(R)
+
+    def check8(got, want, left_out, what):
+        check(got, (want[0], want[1] + 8 * ref.E * left_out), what)
+    sg.sgnn_linear_fwd(ctx(), X, W, b, ACT["gelu"], flags(t), Y, R=R, Z=Z)
+    y, z = ref.linear_fwd(x, w, bb, "gelu", r)
+    p, pu = np.abs(x) @ np.abs(w), np.abs(x) @ np.abs(wu)
+    check8(Z, z, p, "Z"), check8(Y, y, ref.SLOPE * p, "Y")
+    sg.sgnn_glu_fwd(ctx(), X, W, Wu, b, None, ACT["silu"], flags(t), H)
+    h, g, u = ref.glu_fwd(x, w, wu, bb, None, "silu")
+    check8(H, h, ref.SLOPE * p * (np.abs(u[0]) + 1e-3) + pu * (np.abs(g[0]) + 1), "H")
+    dX, dW, dWu, db = torch.full((M, K), 77.0, dtype=dt, device=DEV), *(torch.full((K, N), 77.0, dtype=dt, device=DEV) for _ in range(2)), torch.full((N,), 77.0, device=DEV)
+    sg.sgnn_linear_bwd(ctx(), X, W, Z, ACT["silu"], flags(t), R, dX, dW, db)
+    zz = host(Z)
+    (dx, dws, dbs) = ref.linear_bwd(x, w, zz, "silu", r, t != "fp32")
+    d = ref.SLOPE * np.abs(r)
+    check8(dX, dx, d @ np.abs(w).T, "dX"), check8(dW, dws[0], np.abs(x).T @ d, "dW"), check(db, dbs[0], "db")
+    sg.sgnn_glu_bwd(ctx(), X, W, Wu, Z, H, ACT["silu"], flags(t), R, dX, dW, dWu, dbg=db)
+    hh = host(H)
+    (dx, dws, dbs) = ref.glu_bwd(x, w, wu, zz, hh, "silu", r, t != "fp32")
+    d0, d1 = ref.SLOPE * np.abs(r * hh), np.abs(r) * (np.abs(zz) + 1)
+    check8(dX, dx, d0 @ np.abs(w).T + d1 @ np.abs(wu).T, "dX"), check8(dW, dws[0], np.abs(x).T @ d0, "dWg"), check8(dWu, dws[1], np.abs(x).T @ d1, "dWu"), check(db, dbs[0], "dbg")
+
+
+@pytest.mark.parametrize("shape", [(2304, 200, 130), (2304, 1000, 1000), (40000, 64, 100)], ids=str)
+def test_infinities_and_nan_of_many_rows(shape):
+    M, K, N = shape
+    X, W, Wu = normal((M, K), F32, 1.0, 1), normal((K, N), F32, K ** -0.5, 2), normal((K, N), F32, K ** -0.5, 3)
+    Y, H = torch.empty((M, N), device=DEV), torch.empty((M, N), device=DEV)
+    X[5, K // 2], X[70, 0], X[M - 1, K - 1], X[9, 3] = float("nan"), float("inf"), -float("inf"), 3.4e38
+    sg.sgnn_linear_fwd(ctx(), X, W, None, ACT["relu"], 0, Y)
+    sg.sgnn_glu_fwd(ctx(), X, W, Wu, None, None, ACT["none"], 0, H)
+    rows = np.unique(np.concatenate([[5, 9, 70, M - 1], some(M, 40)]))
+    x, w, wu = host(X[rows]), host(W), host(Wu)
+    with np.errstate(invalid="ignore", over="ignore"):
+        z, u = x @ w, x @ wu
+        want_y, want_h = np.where(np.isnan(z), z, np.maximum(z, 0)), z * u
+    got_y, got_h = host(Y[rows]), host(H[rows])
+    odd = np.isin(rows, [5, 70, M - 1])
+    assert np.isnan(got_y[rows == 5]).all() and np.isnan(got_h[rows == 5]).all()
+    assert np.array_equal(np.isposinf(got_y[odd]), np.isposinf(want_y[odd])) and np.array_equal(np.isnan(got_y[odd]), np.isnan(want_y[odd]))
+    assert np.array_equal(np.isinf(got_h[odd]), np.isinf(want_h[odd])) and np.array_equal(np.isnan(got_h[odd]), np.isnan(want_h[odd]))
+    plain = ~odd & (rows != 9)
+    assert np.isfinite(got_y[plain]).all() and np.isfinite(got_h[plain]).all()
+    big = rows == 9
+    assert np.abs(got_y[big] - want_y[big]).max() <= (K + 12) * ref.E * (np.abs(x[big]) @ np.abs(w)).max()
+
+
+def test_captured_passes_of_many_rows_replay():
+    """The forms of the products that few rows do not reach, captured twice in one graph and replayed between eager calls."""
+    c = sg.Context(0)
+    c.reserve_ffn(40000, 256, 256)
+    B = flags("bf16")
+    X, W, dY, Z, U = normal((33000, 192), BF16, 1.0, 1), normal((192, 200), BF16, 0.07, 2), normal((33000, 200), BF16, 0.1, 3), normal((33000, 200), BF16, 1.0, 4), normal((33000, 200), BF16, 1.0, 5)
+    Xf, Wf, Rf = normal((9000, 192), F32, 1.0, 6), normal((192, 200), F32, 0.07, 7), normal((9000, 200), F32, 1.0, 8)
+    o = [torch.empty(s, dtype=d, device=DEV) for s, d in (((33000, 192), BF16), ((192, 200), BF16), ((192, 200), BF16), ((33000, 192), BF16), ((192, 200), BF16), ((200,), F32),
+                                                          ((9000, 200), F32), ((9000, 200), F32))]
+
+    def run():
+        sg.sgnn_glu_bwd(c, X, W, W, Z, U, ACT["silu"], B, dY, o[0], o[1], o[2])
+        sg.sgnn_linear_bwd(c, X, W, Z, ACT["gelu"], B, dY, o[3], o[4], o[5])
+        sg.sgnn_linear_fwd(c, Xf, Wf, None, ACT["gelu"], 0, o[6], R=Rf, Z=o[7])
+    run()
+    torch.cuda.synchronize()
+    want = [a.clone() for a in o]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+        run()
+    for k in range(3):
+        for a in o:
+            a.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(o, want)), k
+        sg.sgnn_linear_bwd(c, X, W, Z, ACT["relu"], B, dY, o[3], o[4], o[5])
+    c.close()
