@@ -258,3 +258,50 @@ def test_captured_passes_of_many_rows_replay():
         assert all(torch.equal(a, b) for a, b in zip(o, want)), k
         sg.sgnn_linear_bwd(c, X, W, Z, ACT["relu"], B, dY, o[3], o[4], o[5])
     c.close()
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+def test_offsets_past_32_bits(t):
+    """Matrices of more than 2^32 bytes (fp32: 2^33), looked at near their ends; X is zero but for the last rows, so that these alone make the weights' gradients."""
+    M, K, N, last = (1 << 21) + 77, 40, 1032, 900
+    dt = TYPES[t][0]
+    c = sg.Context(0)
+    c.reserve_ffn(M, K, N)
+    W, Wu = normal((K, N), dt, K ** -0.5, 2), normal((K, N), dt, K ** -0.5, 3)
+    X = torch.zeros((M, K), dtype=dt, device=DEV)
+    X[M - last:] = normal((last, K), dt, 1.0, 1)
+    X[:50] = normal((50, K), dt, 1.0, 9)
+    rows = np.unique(np.concatenate([np.arange(50), M - last + some(last, 60)]))
+    x, w, wu = host(X[rows]), host(W), host(Wu)
+    H, G, U = (torch.empty((M, N), dtype=dt, device=DEV) for _ in range(3))
+    sg.sgnn_glu_fwd(c, X, W, Wu, None, None, ACT["silu"], flags(t), H, G=G, U=U)
+    h, g, u = ref.glu_fwd(x, w, wu, None, None, "silu")
+    check(G[rows], g, "G"), check(U[rows], u, "U"), check(H[rows], h, "H")
+    sg.sgnn_linear_fwd(c, X, W, None, ACT["gelu"], flags(t), H, R=U)
+    check(H[rows], ref.linear_fwd(x, w, None, "gelu", host(U[rows]))[0], "Y")
+    G[M // 2:] += 0.5
+    dY = H.mul_(0.01)
+    dX, dW, dWu = torch.empty_like(X), torch.empty_like(W), torch.empty_like(Wu)
+    X[:50] = 0
+    ends = np.arange(M - last, M)
+    gr, ur, dr, xe = host(G[rows]), host(U[rows]), host(dY[rows]), host(X[ends])
+    ge, ue, de = host(G[ends]), host(U[ends]), host(dY[ends])
+    zero = np.zeros((K, N))
+    sg.sgnn_glu_bwd(c, X, W, Wu, G, U, ACT["silu"], flags(t), dY, dX, dW, dWu)
+    check(dX[rows], ref.glu_bwd(np.zeros((len(rows), 1)), w, wu, gr, ur, "silu", dr, t != "fp32")[0], "dX")
+    dws = ref.glu_bwd(xe, zero, zero, ge, ue, "silu", de, t != "fp32")[1]
+    check(dW, dws[0], "dWg"), check(dWu, dws[1], "dWu")
+    db = torch.empty(N, device=DEV)
+    sg.sgnn_linear_bwd(c, X, W, G, ACT["gelu"], flags(t), dY, dX, dW, db)
+    check(dX[rows], ref.linear_bwd(np.zeros((len(rows), 1)), w, gr, "gelu", dr, t != "fp32")[0], "dX")
+    check(dW, ref.linear_bwd(xe, zero, ge, "gelu", de, t != "fp32")[1][0], "dW")
+    n, ir = torch.empty_like(G), torch.empty(M, device=DEV)
+    sg.sgnn_block_norm_fwd(c, U, G, None, None, None, None, 1.0, True, 1e-6, H, n, ir, ir.clone())
+    z = host(G[rows])
+    y = host(U[rows]) + z / np.sqrt((z * z).mean(1, keepdims=True) + 1e-6)
+    want = y / np.sqrt((y * y).mean(1, keepdims=True) + 1e-6)
+    # a handful of fp32 operations an element and sums of N squares, halved by the root
+    tol = (N / 2 + 20) * ref.E * (np.abs(want) + 1)
+    assert np.all(np.abs(host(n[rows]) - want) <= tol + (ref.H * (np.abs(want) + tol) if t != "fp32" else 0))
+    c.close()
+    torch.cuda.empty_cache()
