@@ -262,8 +262,12 @@ template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, 
     a.steps = a.segs * (int)cdiv(a.K, KS);
     const unsigned groups = cdiv(a.M, ROWS);
     const uint32_t tiles = a.strips * groups;
-    // Ranges of the reduction: enough for a workgroup a compute unit, while each wavefront keeps two pieces of its own
-    a.splits = tiles <= 256 ? (uint32_t)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, a.steps / (2 * NW))) : 1;
+    // Ranges of the reduction: up to a workgroup a compute unit (of which two at a time find no room where there are more rows), each wavefront with a piece of its
+    // own, and at most 16 sums to join.  bfloat16, us with up to 512 workgroups and two pieces a wavefront / here: 24 x 4096 x 1024 8.6 / 7.6, 24 x 4096 x 4096 16.4 / 12.5,
+    // 32 x 2048 x 5632 14.8 / 10.4, 1 x 8192 x 8192 28.9 / 26.0 (5.2 TB/s); fp32 24 x 5632 x 1024 16.1 / 11.8, 1 x 8192 x 256 7.9 with 16 ranges, 9.0 with 32.  Two
+    // ranges do not pay their join: 1 x 1024 x 4096 5.7 in one, 6.4 in two.
+    a.splits = (uint32_t)std::max<int64_t>(1, std::min<int64_t>({256 / (int64_t)tiles, a.steps / NW, 16}));
+    if (a.splits == 2 && a.steps < 3 * NW) a.splits = 1;
     a.per_split = (int)cdiv(a.steps, a.splits);
     a.splits = cdiv(a.steps, a.per_split);
     const size_t off = ws->off;
@@ -313,7 +317,7 @@ bool sgnn_ff_rows_take(bool b16, int64_t M, int64_t N, int64_t K, int mats)
     return M <= (b16 ? 32 : 64) || (M <= 2048 && (double)M * (double)N * (double)K * mats <= 8e8);
 }
 
-size_t sgnn_ff_rows_ws_bytes() { return (size_t)512 * 2 * 64 * 64 * 4 + 256; }
+size_t sgnn_ff_rows_ws_bytes() { return (size_t)256 * 2 * 64 * 64 * 4 + 256; }
 
 int sgnn_launch_ff_rows(sgnn_ctx *ctx, int64_t M, int64_t N, int64_t K, int segs, int mats, bool nn, bool b16, const ff_mat *X, const ff_mat *W, const ff_epilogue &e,
                         ws_alloc *ws, hipStream_t st)
