@@ -429,7 +429,13 @@ int tile_for(int pl, int64_t M, int64_t N, int64_t K, int64_t *splits)
     } else if (K >= 2048 && tiles(256, 128) >= 256) return FFT_WIDE;
     if (mid >= 256) return FFT_MID;
     const int64_t n = tiles(64, 128), slices = cdiv(K, pl == 1 ? 64 : 32);
-    if (n <= SGNN_FFN_COUNTS) *splits = std::max<int64_t>(1, std::min<int64_t>(512 / n, slices / 4));
+    // Ranges: up to a workgroup a compute unit, or two where its part is longer than 20 slices: what more of them save is 0.3 us a slice (fp32 0.6), the join costs 4.
+    // us with up to 512 / 256 workgroups, bfloat16: 2500 x 1024 x 256 17.8 / 14.0, 512 x 1024 x 2 x 1024 18.7 / 15.0, 1100 x 4096 x 512 21.2 / 22.2, 2500 x 4096 x 512
+    // 27 / 40; fp32 2500 x 256 x 2 x 256 24.4 / 18.5, 200 x 2048 x 2048 42.6 / 38.5, 512 x 2048 x 2048 42.6 / 44.9, 1100 x 1024 x 1024 32 / 37.
+    if (n <= SGNN_FFN_COUNTS) {
+        *splits = std::max<int64_t>(1, std::min<int64_t>(256 / n, slices / 4));
+        if (slices > 20 * *splits) *splits = std::max<int64_t>(1, std::min<int64_t>(512 / n, slices / 4));
+    }
     return FFT_SMALL;
 }
 

@@ -309,9 +309,10 @@ template <bool NN, int MATS> int launch_kind(sgnn_ctx *ctx, const ffr_args &a, b
 } // namespace
 
 // Which calls these kernels have: the fewest rows always (each weight is read once), more of them while the products are few, since every 64 rows (32
-// gated) read the weights again.  us here / tile kernels, M x K x N, bfloat16: 2048 x 256 x 256 6.2 / 8.4, 512 x 1024 x 1024 9.4 / 16, 1024 x 1024 x 1024 17 / 21,
-// 2048 x 1024 x 1024 31 / 22, 512 x 512 x 2048 13 / 14, 1024 x 512 x 2048 23 / 19, 64 x 4096 x 4096 23 / 21; fp32 (whose tile kernels take parts that are made first):
-// 512 x 1024 x 1024 27 / 34, 1024 x 1024 x 1024 40 / 35, 64 x 4096 x 4096 46 / 62, 100 x 4096 x 4096 72 / 66; gated 512 x 1024 x 2 x 1024 15 / 20, 38 / 36.
+// gated) read the weights again.  us here / tile kernels, M x K x N, bfloat16: 2048 x 256 x 256 6.2 / 7.7, 512 x 1024 x 1024 9.3 / 14.6, 1024 x 1024 x 1024 16.1 / 15.9,
+// 2048 x 1024 x 1024 30 / 15, 512 x 512 x 2048 12.5 / 14.4, 1024 x 512 x 2048 22 / 10, 64 x 4096 x 4096 16.8 / 17.4, 64 x 4096 x 11008 44 / 25; fp32 (whose tile kernels take
+// parts that are made first): 512 x 1024 x 1024 21 / 29, 1024 x 1024 x 1024 40 / 32, 64 x 4096 x 4096 39 / 60, 64 x 4096 x 11008 125 / 155, 100 x 4096 x 4096 64 / 65; gated
+// 512 x 1024 x 2 x 1024 15.7 / 15.8, fp32 37 / 35.
 bool sgnn_ff_rows_take(bool b16, int64_t M, int64_t N, int64_t K, int mats)
 {
     return M <= (b16 ? 32 : 64) || (M <= 2048 && (double)M * (double)N * (double)K * mats <= 8e8);
