@@ -518,14 +518,19 @@ int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
     const int bk = pl == 1 ? 64 : 32;
     const int64_t slices = cdiv(K, bk);
     // The wide tile for long reductions, us WIDE / MID: bfloat16 256 x 1408 x 131072 120 / 130, 1024 x 1024 x 8192 37 / 26; fp32 256 x 1408 x 32768 77 / 75 (not taken
-    // there).  Ranges: as many as fill the chip once.
+    // there).  Ranges: a workgroup a compute unit, or two where its part is longer than 32 slices; every range costs a partial result that is written and read.  us of
+    // product and sum with up to 512 / 256 workgroups, M x N x reduction, bfloat16: 1024 x 1024 x 2500 25.6 / 21.0, 1024 x 1024 x 8192 35.8 / 34.4, 1024 x 2 x 1024 x 8192
+    // 51.6 / 56.8; fp32 256 x 256 x 30000 31.5 / 27.1, 1024 x 2 x 256 x 8192 42.5 / 40.7, 300 x 2 x 700 x 30000 116 / 140.
     auto tiles = [&](int64_t bm, int64_t bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn) * mats; };
-    auto ranges = [&](int64_t n, int64_t total) { return std::max<int64_t>(1, std::min<int64_t>(slices / 4, total / n)); };
+    auto ranges = [&](int64_t n) {
+        auto upto = [&](int64_t total) { return std::max<int64_t>(1, std::min<int64_t>(slices / 4, total / n)); };
+        return slices > 32 * upto(256) ? upto(512) : upto(256);
+    };
     int tile = FFT_SMALL;
-    int64_t splits = ranges(tiles(64, 128), 512);
     const int64_t nw = tiles(256, 256), nm = tiles(128, 128);
-    if (pl == 1 && M > 128 && N > 128 && nw * slices >= 24 * 256) tile = FFT_WIDE, splits = ranges(nw, 256);
-    else if (M > 64 && nm * (slices / 4) >= 192) tile = FFT_MID, splits = ranges(nm, 512);
+    int64_t splits = ranges(tiles(64, 128));
+    if (pl == 1 && M > 128 && N > 128 && nw * slices >= 24 * 256) tile = FFT_WIDE, splits = std::max<int64_t>(1, std::min<int64_t>(slices / 4, 256 / nw));
+    else if (M > 64 && nm * (slices / 4) >= 192) tile = FFT_MID, splits = ranges(nm);
     const size_t off = ws->off;
     const int rc = launch_tile<true, true, FFK_PARTIAL>(ctx, pl, a, tile, splits, ws, st);
     if (rc) return rc;
