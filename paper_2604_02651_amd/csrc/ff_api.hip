@@ -129,11 +129,12 @@ int forward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sgn
         if (rc) return rc;
         return sgnn_launch_ff_nn(ctx, 1, M, N, K, n, x, w, nullptr, nullptr, e, &ws, st);
     }
-    // fp32.  A product of at most 256 tiles of 256 x 128, one a compute unit, with a short K, or of many rows onto few columns: three parts split as X is
+    // fp32.  A product of at most 256 tiles of 256 x 128, one a compute unit, with a short K, or onto few columns: three parts split as X is
     // read and six products (gemm_split.hip) cost less than two parts of X made first, 8 bytes a value at the rate of a copy and two launches, and three
     // products.  With Z and R, parts first against split as read: 32768 x 256 x 256 50 and 44 us, 131072 x 512 x 128 204 and 147, 8192 x 256 x 512 38
-    // and 27; past the rule 131072 x 256 x 256 171 and 196, 32768 x 256 x 512 67 and 86, 4096 x 2048 x 256 48 and 71
-    if (n == 1 && K >= 4 && N >= 4 && ((K <= 512 && ((M + 255) / 256) * ((N + 127) / 128) <= 256) || (N <= 128 && M >= 16384))) {
+    // and 27, 15167 x 3762 x 27 194 and 90, 2500 x 1024 x 64 31 and 17; past the rule 131072 x 256 x 256 171 and 196, 32768 x 256 x 512 67 and 86, 4096 x 2048 x 256
+    // 48 and 71
+    if (n == 1 && K >= 4 && N >= 4 && ((K <= 512 && ((M + 255) / 256) * ((N + 127) / 128) <= 256) || N <= 128)) {
         const sgnn_split_epilogue se = {1, act, R ? static_cast<const float *>(R->ptr) : nullptr, R ? R->ld : 0, Z[0] ? static_cast<float *>(Z[0]->ptr) : nullptr, Z[0] ? Z[0]->ld : 0};
         return sgnn_launch_gemm_split(ctx, 0, 0, M, N, K, static_cast<const float *>(X->ptr), X->ld, nullptr, static_cast<const float *>(W[0]->ptr), W[0]->ld, b[0], 0,
                                       static_cast<float *>(Y->ptr), Y->ld, nullptr, 0, nullptr, &ws, st, &se);

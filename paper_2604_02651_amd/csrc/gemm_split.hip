@@ -391,7 +391,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_split_kernel(split_args 
                 if (!plain && a.relu) z[e] = fmaxf(z[e], 0.f);
                 if (!plain && a.mask && !(m[p][e] > 0.f)) z[e] = 0.f;
             }
-            if (a.e.used) {
+            if (!plain && a.e.used) {
                 if (a.e.Z) store(a.e.Z + (m0 + r) * a.e.ldz + col);
                 ff_with_act(a.e.act, [&](auto act) {
 #pragma unroll
@@ -431,6 +431,22 @@ int launch_split(sgnn_ctx *ctx, int ta, int tb, split_args a, hipStream_t st)
     SGNN_SPLIT_CASE(true, false, true)
 #undef SGNN_SPLIT_CASE
     return sgnn_fail(ctx, SGNN_ERR_UNSUPPORTED, "sgnn_gemm: trans_a and trans_b together are not implemented");
+}
+
+// The sum of the ranges' products in their order, and the epilogue of a feed-forward operator
+__global__ __launch_bounds__(256) void split_epilogue_kernel(split_args a)
+{
+    const int64_t n = a.M * a.N;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / a.N, col = i - row * a.N;
+        float z = 0.f;
+#pragma unroll 8
+        for (uint32_t s = 0; s < a.splits; ++s) z += a.partial[(int64_t)s * n + i];
+        if (a.bias) z += a.bias[col];
+        if (a.e.Z) a.e.Z[row * a.e.ldz + col] = z;
+        ff_with_act(a.e.act, [&](auto act) { z = ff_act<decltype(act)::value>(z); });
+        a.C[row * a.ldc + col] = a.e.R ? z + a.e.R[row * a.e.ldr + col] : z;
+    }
 }
 
 } // namespace
@@ -503,13 +519,26 @@ int sgnn_launch_gemm_split(sgnn_ctx *ctx, int ta, int tb, int64_t M, int64_t N, 
         } else if (!ws->ok)
             return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "sgnn_gemm: scratch too small for the split reduction: call sgnn_ctx_reserve");
     }
+    // With an epilogue, which a kernel of its own then applies: a slice of the reduction takes 1.1 us where a tile is alone on its compute unit, so a long one
+    // onto few narrow tiles is split into eight ranges (one for each XCD, see above), or sixteen.  us in one range / here: 8192 x 64 x 2048 72 / 37, 15167 x 64 x 1024
+    // 53 / 40, 2500 x 128 x 1024 32 / 22; with 469 tiles, 30000 x 64 x 2048, 86 / 112.
+    if (e && !ta && bn == 64 && tiles <= 256 && K >= 768) {
+        a.kps = (int64_t)cdiv(cdiv(K, tiles < 64 && K >= 2048 ? 16 : 8), SBK) * SBK;
+        a.splits = cdiv(K, a.kps);
+        a.partial = ws->get<float>((size_t)a.splits * M * N);
+        if (!ws->ok) return sgnn_fail(ctx, SGNN_ERR_CAPACITY, "feed-forward operator: scratch too small: call sgnn_ctx_reserve_ffn");
+    }
     int rc;
     if (bm == 256) rc = launch_split<256, 128, 4, 2>(ctx, ta, tb, a, st);
     else if (bn == 128) rc = launch_split<128, 128, 2, 4>(ctx, ta, tb, a, st);
     else if (bm == 128) rc = launch_split<128, 64, 2, 2>(ctx, ta, tb, a, st);
     else rc = launch_split<64, 64, 2, 2>(ctx, ta, tb, a, st);
     if (rc) return rc;
-    if (a.splits > 1) {
+    if (a.splits > 1 && e) {
+        const dim3 grid((unsigned)std::min<int64_t>(cdiv(M * N, 256), 1 << 16));
+        SGNN_LAUNCH(ctx, st, "split_epilogue_kernel", SGNN_TAG, split_epilogue_kernel, grid, dim3(256), 0, st, a);
+        ws->off = ws_off;
+    } else if (a.splits > 1) {
         rc = sgnn_launch_splitk_reduce(ctx, a.partial, (int)a.splits, M, N, C, ldc, cs_partial, cs_partial ? b_colsum : nullptr, st);
         ws->off = ws_off;      // what the caller launches next on this stream may have the scratch
     }

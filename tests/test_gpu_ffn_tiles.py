@@ -305,3 +305,27 @@ def test_offsets_past_32_bits(t):
     assert np.all(np.abs(host(n[rows]) - want) <= tol + (ref.H * (np.abs(want) + tol) if t != "fp32" else 0))
     c.close()
     torch.cuda.empty_cache()
+
+
+# fp32 onto few columns: the reduction split into ranges, each with its epilogue
+@pytest.mark.parametrize("a", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("shape", [(2500, 1000, 27), (2051, 2100, 128), (4099, 769, 4), (8191, 3762, 64), (8193, 900, 65), (15167, 1031, 31), (16400, 800, 100)], ids=str)
+def test_long_reductions_onto_few_columns(shape, a):
+    M, K, N = shape
+    print(shape, a, flush=True)
+    X, W, b = padded(normal((M, K), F32, 1.0, 1), 3), padded(normal((K, N), F32, K ** -0.5, 2), 1), normal((N,), F32, 0.3, 5)
+    Y, Z = (padded(torch.full((M, N), 77.0, device=DEV), 5) for _ in range(2))
+    Y.copy_(normal((M, N), F32, 1.0, 4))
+    rows = some(M)
+    y, z = ref.linear_fwd(host(X[rows]), host(W), host(b), a, host(Y[rows]))
+    sg.sgnn_linear_fwd(ctx(), X, W, b, ACT[a], 0, Y, R=Y, Z=Z)          # the residual in place
+    check(Z[rows], z, "Z"), check(Y[rows], y, "Y")
+    assert torch.isnan(Y.as_strided((M, 5), (N + 5, 1), N)).all() and torch.isnan(Z.as_strided((M, 5), (N + 5, 1), N)).all()
+    sg.sgnn_linear_fwd(ctx(), X, W, None, ACT[a], 0, Y)
+    check(Y[rows], ref.linear_fwd(host(X[rows]), host(W), None, a, None)[0], "Y")
+    if K >= 1000 and N > 4:
+        small = sg.Context(0)
+        with pytest.raises(sg.SgnnError) as e:
+            sg.sgnn_linear_fwd(small, X, W, None, ACT[a], 0, Y)
+        assert e.value.code == -2
+        small.close()
