@@ -25,7 +25,7 @@ struct ffr_args {
     int segs;
     ff_mat X[2], W[2];                // of each segment, or projection
     ff_epilogue e;
-    uint32_t strips, splits;
+    uint32_t strips, splits, groups;  // groups: of ROWS rows
     int steps, per_split;             // pieces along the whole reduction, and of one range
     float *partial;                   // [strips][splits][MATS][16 RT][CB]
     uint32_t *arrived;                // [strips], zero between calls
@@ -41,10 +41,12 @@ template <int KIND, bool NN, int V, int RT, int MATS> __global__ __launch_bounds
     __shared__ float red[MATS][NW][ROWS][CB];
     __shared__ uint32_t last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, kg = lane >> 4;
-    const uint32_t total = a.strips * a.splits, run = (total + 7) / 8, id = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
+    // each XCD has a run of the work, the row groups of a piece of the weights after each other
+    const uint32_t total = a.strips * a.splits * a.groups, run = (total + 7) / 8, id = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= run || id >= total) return;
-    const uint32_t strip = id / a.splits, split = id % a.splits;
-    const int row0 = blockIdx.y * ROWS, n0 = (int)strip * CB;
+    const uint32_t rest = a.groups > 1 ? id / a.groups : id, group = id - rest * a.groups;
+    const uint32_t strip = a.splits > 1 ? rest / a.splits : rest, split = rest - strip * a.splits;
+    const int row0 = (int)group * ROWS, n0 = (int)strip * CB;
     const int s_end = min(a.steps, (int)(split + 1) * a.per_split), seg_steps = (int)((a.K + KS - 1) / KS);
 
     struct piece { uint32_t x[RT][KL * (KIND == FFR_F32 ? 4 : 2) / 4], w[MATS][WD]; };
@@ -199,7 +201,7 @@ template <int KIND, bool NN, int V, int RT, int MATS> __global__ __launch_bounds
                 for (int r = 0; r < 4; ++r) red[q][wave][16 * t + 4 * kg + r][NN ? V * i + c : 16 * c + i] = acc[q][t][c][r];
     __syncthreads();
     const int rows = min(a.M - row0, ROWS);
-    const uint32_t tile = blockIdx.y * a.strips + strip;
+    const uint32_t tile = group * a.strips + strip;
     if (a.splits > 1) {
         float *to = a.partial + (size_t)(tile * a.splits + split) * (MATS * ROWS * CB);
         for (int j = threadIdx.x; j < MATS * rows * CB; j += 64 * NW) {
@@ -260,8 +262,8 @@ template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, 
     constexpr int KS = KIND == FFR_F32 ? 16 : 32, CB = 16 * V, NW = rows_waves<V, RT, MATS>(), ROWS = 16 * RT;
     a.strips = cdiv(a.N, CB);
     a.steps = a.segs * (int)cdiv(a.K, KS);
-    const unsigned groups = cdiv(a.M, ROWS);
-    const uint32_t tiles = a.strips * groups;
+    a.groups = cdiv(a.M, ROWS);
+    const uint32_t tiles = a.strips * a.groups;
     // Ranges of the reduction: up to a workgroup a compute unit (of which two at a time find no room where there are more rows), each wavefront with a piece of its
     // own, and at most 16 sums to join.  bfloat16, us with up to 512 workgroups and two pieces a wavefront / here: 24 x 4096 x 1024 8.6 / 7.6, 24 x 4096 x 4096 16.4 / 12.5,
     // 32 x 2048 x 5632 14.8 / 10.4, 1 x 8192 x 8192 28.9 / 26.0 (5.2 TB/s); fp32 24 x 5632 x 1024 16.1 / 11.8, 1 x 8192 x 256 7.9 with 16 ranges, 9.0 with 32.  Two
@@ -281,7 +283,7 @@ template <int KIND, bool NN, int V, int RT, int MATS> int launch(sgnn_ctx *ctx, 
     char tag[56] = "";
     if (ctx->prof_on) snprintf(tag, sizeof(tag), "%s%s %dx%dx%lld /%u", NN ? "NN" : "NT", MATS > 1 ? " gated" : "", a.M, a.N, (long long)a.K, a.splits);
     auto run = [&]() -> int {
-        SGNN_LAUNCH(ctx, st, "ff_rows_kernel", tag, (ff_rows_kernel<KIND, NN, V, RT, MATS>), dim3((a.strips * a.splits + 7) / 8 * 8, groups), dim3(64 * NW), 0, st, a);
+        SGNN_LAUNCH(ctx, st, "ff_rows_kernel", tag, (ff_rows_kernel<KIND, NN, V, RT, MATS>), dim3((tiles * a.splits + 7) / 8 * 8), dim3(64 * NW), 0, st, a);
         return SGNN_OK;
     };
     int rc = run();
