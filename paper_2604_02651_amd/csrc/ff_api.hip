@@ -280,7 +280,26 @@ int backward(sgnn_ctx *ctx, const char *name, int n, const sgnn_mat *X, const sg
         if (rc) return rc;
         return sgnn_launch_ff_nt(ctx, 1, M, K, N, n, d, w, nullptr, nullptr, view(dX), &ws, st);
     }
-    // fp32: the gradients' rows are scaled by themselves, the rows of X so that with the gradients' all products have one scale (ff_gemm.hip)
+    // fp32.  One matrix of weights and few multiplications, or few columns: D as it is, both products by the kernel that splits what it reads (gemm_split.hip), the one for
+    // the weights with the column sums of D; three launches fewer.  us of all kernels, parts made first / split as read, M x K x N: 100 x 256 x 256 32 / 21,
+    // 1200 x 1024 x 256 58 / 47, 2500 x 256 x 256 46 / 31, 30000 x 256 x 256 98 / 88, 100000 x 64 x 64 86 / 58, 100000 x 1536 x 90 805 / 625; past the rule 2500 x 1024 x 256
+    // 52 / 67, 1200 x 1024 x 1024 65 / 97, 30000 x 200 x 531 148 / 199, 10000 x 1536 x 90 94 / 98
+    if (n == 1 && M >= 4 && K >= 4 && N >= 4 && ((double)M * (double)K * (double)N <= 5e8 || (K <= 256 && N <= 256) || (N <= 128 && M >= 16384))) {
+        float *const sums = any_dw ? db[0] : nullptr;          // the product for the weights has them as well
+        if (!is_dy || (db[0] && !any_dw)) {
+            float *const none[1] = {any_dw ? nullptr : db[0]};
+            rc = sgnn_launch_ff_act_bwd(ctx, M, N, np, act, view(dY), z0, nullptr, is_dy ? ff_mat{nullptr, 0, 0} : d0, nullptr, none, &ws, st);
+        }
+        const float *const d = static_cast<const float *>(D);
+        if (!rc && any_dw)
+            rc = sgnn_launch_gemm_split(ctx, 1, 0, K, N, M, static_cast<const float *>(X->ptr), X->ld, nullptr, d, ldd, nullptr, 0, static_cast<float *>(dW[0]->ptr), dW[0]->ld, nullptr, 0,
+                                        sums, &ws, st);
+        if (rc || !dX) return rc;
+        if (few) return few_rows();
+        return sgnn_launch_gemm_split(ctx, 0, 1, M, K, N, d, ldd, nullptr, static_cast<const float *>(W[0]->ptr), W[0]->ld, nullptr, 0, static_cast<float *>(dX->ptr), dX->ld, nullptr, 0,
+                                      nullptr, &ws, st);
+    }
+    // The gradients' rows are scaled by themselves, the rows of X so that with the gradients' all products have one scale (ff_gemm.hip)
     const bool tiles_dx = dX && !few, split = any_dw || tiles_dx;
     // the gradients as parts at once where nothing else reads them and a row fits the registers
     const unsigned in_registers = split && !few && !is_dy ? sgnn_ff_act_bwd_parts_groups(M, np) : 0;

@@ -498,12 +498,12 @@ int sgnn_launch_ff_nt(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, in
     return rc;
 }
 
-// Scratch of the products: partial results of tn (at most 512 ranges; over all of them 256 tiles of 256 x 256, or as many elements in others, or one result),
-// sums of split tiles (512 of 64 x 128)
+// Scratch of the products: partial results of tn (at most 512 ranges; over all of them 512 tiles of 128 x 128, or as many elements in others, or one result), sums of
+// split tiles (512 of 64 x 128); of gemm_split.hip 768 tiles of up to 256 x 128 and the column sums that ride along
 size_t sgnn_ff_gemm_ws_bytes(uint64_t d_in, uint64_t d_out)
 {
     const uint64_t results = 2 * d_in * d_out;
-    return std::max<uint64_t>(std::min<uint64_t>(512 * results, std::max<uint64_t>(256ull * 65536, results)), 512ull * 64 * 128) * 4 + 512;
+    return std::max<uint64_t>(std::min<uint64_t>(512 * results, std::max<uint64_t>(768ull * 32768 + (1 << 18), results)), 512ull * 64 * 128) * 4 + 512;
 }
 
 int sgnn_launch_ff_tn(sgnn_ctx *ctx, int pl, int64_t M, int64_t N, int64_t K, int mats, const ff_op &A, const ff_op *B, const int32_t *ex_rows, const int32_t *ex,
