@@ -6,7 +6,7 @@
 //   ds = sum over the rows of t w b;  dgamma_post of v zh;  dgamma_pre of dN yh
 //
 // Every matrix is read or written once, which is what bounds these kernels.  A group of G lanes owns a row and keeps it in registers, V values
-// (16 bytes) a lane and chunk, CH chunks: G from 16 lanes (four rows a wavefront: 256 bfloat16 columns would leave half of a whole wavefront idle) to a
+// (16 bytes) a lane and chunk, CH chunks: G from 8 lanes (eight rows a wavefront: 256 bfloat16 columns would leave half of a whole wavefront idle) to a
 // workgroup of 1024 threads.  Row sums are exchanges inside the wavefront, and through LDS between the wavefronts of a row.  Column sums stay in
 // registers over all rows of a group, the groups of a workgroup meet in LDS, every workgroup writes one partial sum a column and a second kernel
 // adds these in a fixed order: bit-reproducible.  N is taken from y before it is rounded for storage; statistics and sums are fp32.
@@ -308,14 +308,21 @@ __global__ __launch_bounds__(1024) void block_norm_sums_kernel(const float *__re
 
 constexpr int MAX_D = 16384, BWD_GROUPS = 1024, FWD_GROUPS = 4096;
 
-// lanes of a row and chunks of a lane by the row's chunks: the fewest lanes that hold it, one chunk each up to a wavefront
-template <int T, int V, class F> int with_shape(int d, F f)
+// Lanes of a row and chunks of a lane by the row's chunks: the fewest lanes that hold it, one chunk each up to a wavefront.  What is behind a row's end costs as
+// much as the rest: 541291 x 64 bfloat16 114 us with 16 lanes a row, 73 with 8, backward 193 and 118; fp32 rows of 129 to 192 chunks by 64 lanes of three instead of
+// 256 of one, 150000 x 704 347 and 327, backward 825 and 705, but 5.0 and 6.3 for 400 rows, where a row's own time counts.  (513 to 768 chunks by 256 lanes of
+// three are not faster: 30000 x 2536 300 and 306, backward 637 and 697.)
+template <int T, int V, class F> int with_shape(int d, int64_t rows, F f)
 {
     const int chunks = (d + V - 1) / V;
+    if (chunks <= 8) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
     if (chunks <= 16) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
     if (chunks <= 32) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
     if (chunks <= 64) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
     if (chunks <= 128) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 64>());
+    if constexpr (V == 4) {
+        if (chunks <= 192 && rows >= 2048) return f(std::integral_constant<int, 3>(), std::integral_constant<int, 64>());
+    }
     if (chunks <= 256) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 256>());
     if (chunks <= 512) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 256>());
     if (chunks <= 1024) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1024>());
@@ -327,7 +334,7 @@ template <int T, int V, class F> int with_shape(int d, F f)
 
 template <int T, int V> int launch_fwd(sgnn_ctx *ctx, const ff_norm &a, hipStream_t st)
 {
-    return with_shape<T, V>(a.d, [&](auto ch, auto g) -> int {
+    return with_shape<T, V>(a.d, a.rows, [&](auto ch, auto g) -> int {
         constexpr int CH = decltype(ch)::value, G = decltype(g)::value, RPW = threads<G>() / G;
         SGNN_LAUNCH(ctx, st, "block_norm_fwd_kernel", SGNN_TAG, (block_norm_fwd_kernel<T, V, CH, G>), dim3((unsigned)std::min<int64_t>(cdiv(a.rows, RPW), FWD_GROUPS)), dim3(threads<G>()), 0, st, a);
         return SGNN_OK;
@@ -336,7 +343,7 @@ template <int T, int V> int launch_fwd(sgnn_ctx *ctx, const ff_norm &a, hipStrea
 
 template <int T, int V> int launch_bwd(sgnn_ctx *ctx, const ff_norm &a, ws_alloc *ws, hipStream_t st)
 {
-    return with_shape<T, V>(a.d, [&](auto ch, auto g) -> int {
+    return with_shape<T, V>(a.d, a.rows, [&](auto ch, auto g) -> int {
         constexpr int CH = decltype(ch)::value, G = decltype(g)::value, RPW = threads<G>() / G;
         const bool sums = a.dgamma_post || a.dscale || a.dgamma_pre;
         const unsigned grid = (unsigned)std::min<int64_t>(std::max<int64_t>(cdiv(a.rows, RPW), 1), BWD_GROUPS);

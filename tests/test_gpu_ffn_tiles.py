@@ -329,3 +329,42 @@ def test_long_reductions_onto_few_columns(shape, a):
             sg.sgnn_linear_fwd(small, X, W, None, ACT[a], 0, Y)
         assert e.value.code == -2
         small.close()
+
+
+# norms of widths on either side of every change of the lanes a row has
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(3001, 30), (3001, 32), (3001, 33), (3001, 64), (3001, 65), (2048, 513), (2051, 704), (2047, 704), (2500, 768), (2500, 769)], ids=str)
+def test_norms_of_many_rows(shape, t):
+    M, d = shape
+    dt = TYPES[t][0]
+    X, Z, gate, dY, dN = (normal((M, d), dt, 1.0, i) for i in range(1, 6))
+    gp, sc, gn = (normal((d,), F32, 0.5, i) for i in range(6, 9))
+    Y, N, irp, irn = torch.empty_like(X), torch.empty_like(X), torch.empty(M, device=DEV), torch.empty(M, device=DEV)
+    sg.sgnn_block_norm_fwd(ctx(), X, Z, gate, gp, sc, gn, 0.5, True, 1e-6, Y, N, irp, irn)
+    o = [torch.empty_like(X) for _ in range(3)]
+    g = [torch.empty(d, device=DEV) for _ in range(3)]
+    sg.sgnn_block_norm_bwd(ctx(), Z, Y, gate, gp, sc, gn, 0.5, True, irp, irn, dY, dN, o[0], o[1], o[2], g[0], g[1], g[2])
+    # the formulas in float64 by torch, y as it was stored
+    x, z, w = X.double(), Z.double(), torch.sigmoid(gate.double())
+    zh = z / torch.sqrt((z * z).mean(1, keepdim=True) + 1e-6)
+    y = 0.5 * x + sc.double() * w * gp.double() * zh
+    half = ref.H if t == "bf16" else ref.E
+    # sums of d squares halved by the root, a dozen operations an element, and the rounding as it is stored
+    rel = (d / 2 + 20) * ref.E + half
+    assert float(((Y.double() - y).abs() / (y.abs() + (0.5 * x).abs() + 1)).max()) <= rel
+    nn = gn.double() * y / torch.sqrt((y * y).mean(1, keepdim=True) + 1e-6)
+    assert float(((N.double() - nn).abs() / (nn.abs() + 1)).max()) <= 3 * rel
+    ys, ir = Y.double(), irn.double()[:, None]
+    yh, q = ys * ir, dN.double() * gn.double()
+    t_ = dY.double() + ir * (q - yh * (q * yh).mean(1, keepdim=True))
+    big = 1 + t_.abs() + (q * ir).abs()
+    assert float(((o[0].double() - 0.5 * t_).abs() / big).max()) <= 3 * rel
+    h = t_ * sc.double() * w * gp.double()
+    dz = irp.double()[:, None] * (h - zh * (h * zh).mean(1, keepdim=True))
+    assert float(((o[1].double() - dz).abs() / (1 + dz.abs() + (irp.double()[:, None] * h.abs() * (1 + zh.abs())))).max()) <= 6 * rel
+    dg = h * zh * (1 - w)
+    assert float(((o[2].double() - dg).abs() / (1 + dg.abs() + (h * zh).abs())).max()) <= 6 * rel
+    # sums over M rows: each term to a few roundings of fp32, the sum itself to M of them
+    for got, term in ((g[0], t_ * sc.double() * w * zh), (g[1], t_ * w * gp.double() * zh), (g[2], dN.double() * yh)):
+        want, mag = term.sum(0), term.abs().sum(0) + M * 1e-3
+        assert float(((got.double() - want).abs() / mag).max()) <= (M + 2 * d + 60) * ref.E
